@@ -279,7 +279,11 @@ typedef enum {
     ELSA_KERNEL_BLOCK_ROWWISE = 13,     /* LayerNorm, residual add, GELU, column copy of the chained block */
     ELSA_KERNEL_BACKWARD_FORMAT = 14,   /* transposes, column sums and mask of the backward pass */
     ELSA_KERNEL_ATTENTION = 15,         /* multi-head self-attention of the chained block */
-    ELSA_KERNEL_LINEAR_SMALL = 16       /* linear with few token rows, straight from the packed weight */
+    ELSA_KERNEL_LINEAR_SMALL = 16,      /* linear with few token rows, straight from the packed weight */
+    ELSA_KERNEL_NORM_BACKWARD = 17,     /* gradient of LayerNorm and its column sums */
+    ELSA_KERNEL_ROTARY = 18,            /* rotary positions */
+    ELSA_KERNEL_PACKED_ATTENTION = 19,  /* attention over packed sequences, and its plan */
+    ELSA_KERNEL_PACKED_ATTENTION_BACKWARD = 20
 } elsa_kernel_id;
 
 typedef struct {
@@ -516,6 +520,103 @@ size_t elsa_backward_workspace_bytes(int rows, int in, int out, int N, int M, el
 elsa_status elsa_nm_linear_backward(const void* dY, const void* X, int rows, const void* vals, const uint32_t* idx,
                                     int out, int in, int N, int M, elsa_dtype dtype, void* dX, void* dW, void* db,
                                     void* workspace, size_t workspace_bytes, uint32_t* dev_status, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * What stands between the pruned linears of a block when it is trained (Alg. 2), or when it takes images of many sizes,
+ * video or causal sequences: LayerNorm with its gradient, rotary positions, attention over packed sequences with its
+ * gradient.  16-bit tensors of one dtype, fp32 arithmetic, one rounding of each stored value; no atomics on results: the
+ * same inputs give the same bits every time.  DEVICE pointers, 16-byte aligned, unless stated otherwise; asynchronous on
+ * `stream`; errors as for elsa_nm_linear.
+ *
+ * LayerNorm of rows of dim values (a multiple of 8):
+ *     s = x + residual (rounded to dtype; without a residual s is x)
+ *     y = (s - mean) / sqrt(var + eps) * gain + bias      mean and biased variance over the row s as stored
+ * residual, s: both given or both NULL; s may be x's or residual's own buffer, y may be x's where there is no residual.
+ * stats: [rows][2] floats, mean and 1 / sqrt(var + eps), for the gradient; or NULL.
+ */
+elsa_status elsa_layer_norm(const void* x, const void* residual, const void* gain, const void* bias, int rows, int dim,
+                            float eps, elsa_dtype dtype, void* s, void* y, float* stats, void* stream);
+/*
+ * Its gradient, dy arriving at y and ds (or NULL) along the residual path at s:
+ *     dx [rows][dim] = ds + d(y)/d(s) dy  (the gradient of x and of the residual alike)
+ *     dgain [dim] = sum over rows of dy (s - mean) / sqrt(var + eps)      dbias [dim] = sum over rows of dy
+ * Any of dx, dgain, dbias may be NULL (not computed).  dx may be dy's or ds's own buffer.  dim <= 16384.  workspace:
+ * elsa_layer_norm_backward_workspace_bytes(...) bytes, 256-byte aligned (partial column sums); not needed, and may be
+ * NULL, without dgain and dbias.
+ */
+size_t elsa_layer_norm_backward_workspace_bytes(int rows, int dim);
+elsa_status elsa_layer_norm_backward(const void* dy, const void* s, const float* stats, const void* gain, const void* ds,
+                                     int rows, int dim, elsa_dtype dtype, void* dx, void* dgain, void* dbias,
+                                     void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Rotary positions.  A head of head_dim values is head_dim / 2 pairs; the pairs are dealt out to `axes` axes in
+ * `sections` of pairs, and pair number i of an axis' n turns by the row's position on that axis times base^(-i / n)
+ * radians (shared: pair p of the head by base^(-p / (head_dim / 2)), one range of rates over all axes):
+ *     (a, b) -> (a cos - b sin, b cos + a sin)      inverse: by minus the angle, which is the gradient too
+ * A pair is values (2p, 2p + 1) of the head (interleaved) or (p, p + head_dim / 2).  Any int32 position, negative ones
+ * too, is as exact as a small one: angles are kept as 64-bit fractions of a turn.
+ * elsa_rotary_make_plan is HOST arithmetic (head_dim a multiple of 16 up to 256, 1 <= base); the plan holds no pointers.
+ * elsa_rotary turns `heads` adjacent heads of each row (the query and the key heads of qkv in one call): x rows are
+ * x_pitch values apart, y rows y_pitch (multiples of 8, at least heads * head_dim); positions: [rows][axes].  y may be
+ * x's own buffer with the same pitch; otherwise they may not overlap.
+ */
+#define ELSA_ROTARY_MAX_AXES 4
+#define ELSA_ROTARY_MAX_PAIRS 128
+typedef struct {
+    int head_dim, axes, interleaved;
+    unsigned char axis[ELSA_ROTARY_MAX_PAIRS]; /* of each pair */
+    uint64_t turns[ELSA_ROTARY_MAX_PAIRS];     /* of each pair: turns per position, times 2^64 */
+} elsa_rotary_plan;
+elsa_status elsa_rotary_make_plan(int head_dim, const int* sections, int axes, double base, int shared, int interleaved,
+                                  elsa_rotary_plan* plan);
+elsa_status elsa_rotary(const void* x, long long x_pitch, const int32_t* positions, const elsa_rotary_plan* plan, int rows,
+                        int heads, int inverse, elsa_dtype dtype, void* y, long long y_pitch, void* stream);
+
+/*
+ * Attention over packed sequences: the rows of q, k and v hold sequences of any lengths one after another, sequence i in
+ * rows [offsets[i], offsets[i + 1]) (offsets: int32 [sequences + 1], device, not decreasing, within 0 .. rows; empty
+ * sequences are allowed; rows before the first and behind the last belong to none).
+ *     a[r, h] = sum over j of p_j v[j, h / group],   p = softmax over j of scale * q[r, h] . k[j, h / group]
+ * over the rows j of r's own sequence, causal: those up to r; group = heads / kv_heads query heads share a key head.
+ * Rows of no sequence are neither read nor written.  Non-finite values of one sequence reach no other; inside a sequence
+ * one in v, or in da, may reach every row of it, a causal mask or not.
+ *
+ * elsa_packed_plan cuts the sequences into tiles once for any number of calls with the same offsets (all layers, both
+ * directions): plan is elsa_packed_plan_bytes(...) of device memory that the calls read.  Offsets that break the rules
+ * make an empty plan, and dev_status (if given) receives ELSA_ERR_SHAPE | 69 << 8; a plan made for other rows or another
+ * number of sequences makes a call that computes nothing, ELSA_ERR_SHAPE | 79 << 8.
+ * q [rows][heads * head_dim], k and v [rows][kv_heads * head_dim]: heads side by side in a row, rows *_pitch values apart
+ * (so the thirds of a qkv tensor are taken as they lie); head_dim 32, 64 or 128; pitches multiples of 8.
+ * lse (or NULL; needed for the gradient): fp32 [heads][rows], log of the sum of exp(scale * q . k).  Scores, sums and
+ * outputs are kept in fp32; the probabilities, and in the gradient ds, are rounded to dtype for the tensor cores.
+ */
+typedef struct {
+    const void* q;
+    const void* k;
+    const void* v;
+    long long q_pitch, k_pitch, v_pitch;
+    int rows, heads, kv_heads, head_dim;
+    int causal;
+    float scale;
+} elsa_packed_qkv;
+size_t elsa_packed_plan_bytes(int rows, int sequences);
+elsa_status elsa_packed_plan(const int32_t* offsets, int sequences, int rows, void* plan, size_t plan_bytes,
+                             uint32_t* dev_status, void* stream);
+elsa_status elsa_packed_attention(const elsa_packed_qkv* in, elsa_dtype dtype, const void* plan, int sequences, void* a,
+                                  long long a_pitch, float* lse, uint32_t* dev_status, void* stream);
+/*
+ * The gradient, da arriving at a: dq like q, dk and dv like k and v (rows dq_pitch, dk_pitch, dv_pitch values apart, so
+ * they may be the thirds of one tensor), sums over the query heads of a key head included.  a and lse: the forward
+ * call's.  workspace: elsa_packed_attention_workspace_bytes(rows, heads) bytes, 256-byte aligned.  Outputs may not overlap
+ * inputs.
+ */
+size_t elsa_packed_attention_workspace_bytes(int rows, int heads);
+elsa_status elsa_packed_attention_backward(const elsa_packed_qkv* in, elsa_dtype dtype, const void* plan, int sequences,
+                                           const void* a, long long a_pitch, const float* lse, const void* da,
+                                           long long da_pitch, void* dq, long long dq_pitch, void* dk, long long dk_pitch,
+                                           void* dv, long long dv_pitch, void* workspace, size_t workspace_bytes,
+                                           uint32_t* dev_status, void* stream);
 
 /*
  * Test hook for the device-side failure path.  Every wait of the tensor-core kernels is bounded: a wait that

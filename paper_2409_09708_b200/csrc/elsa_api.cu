@@ -1718,6 +1718,143 @@ int elsa_profile_stop(elsa_kernel_time* records, int capacity)
 
 unsigned long long elsa_launch_count(void) { return g_launches.load(std::memory_order_relaxed); }
 
+elsa_status elsa_layer_norm(const void* x, const void* residual, const void* gain, const void* bias, int rows, int dim, float eps,
+                            elsa_dtype dtype, void* s, void* y, float* stats, void* stream)
+{
+    if (!x || !gain || !bias || !y) return fail(ELSA_ERR_NULL, "x, gain, bias and y must not be NULL");
+    if ((residual == nullptr) != (s == nullptr)) return fail(ELSA_ERR_NULL, "residual and s go together");
+    if (dtype != ELSA_F16 && dtype != ELSA_BF16) return fail(ELSA_ERR_DTYPE, "dtype %d is neither ELSA_F16 nor ELSA_BF16", (int)dtype);
+    if (rows <= 0 || dim <= 0) return fail(ELSA_ERR_SHAPE, "non-positive dimension (rows=%d, dim=%d)", rows, dim);
+    if (!(eps >= 0.f)) return fail(ELSA_ERR_SHAPE, "eps=%g must not be negative", (double)eps);
+    if (dim % 8 != 0) return fail(ELSA_ERR_ALIGN, "dim=%d must be a multiple of 8 (16-byte row pitch)", dim);
+    if (!aligned16(x) || !aligned16(residual) || !aligned16(gain) || !aligned16(bias) || !aligned16(s) || !aligned16(y) || ((uintptr_t)stats & 7u))
+        return fail(ELSA_ERR_ALIGN, "x, residual, gain, bias, s and y must be 16-byte aligned, stats 8-byte aligned");
+    const uint16_t *A = (const uint16_t*)x, *R = (const uint16_t*)residual, *g = (const uint16_t*)gain, *b = (const uint16_t*)bias;
+    if (layer_norm_rows_suits(dim) || !layer_norm_columns_suits(dim))
+        return launch_layer_norm(A, R, (uint16_t*)s, g, b, (uint16_t*)y, rows, dim, eps, dtype, (cudaStream_t)stream, nullptr, stats);
+    return launch_layer_norm_columns(A, R, (uint16_t*)s, g, b, (uint16_t*)y, stats, rows, dim, eps, dtype, (cudaStream_t)stream);
+}
+
+size_t elsa_layer_norm_backward_workspace_bytes(int rows, int dim)
+{
+    return rows <= 0 || dim <= 0 || dim % 8 != 0 || !layer_norm_columns_suits(dim) ? 0 : layer_norm_backward_workspace(rows, dim);
+}
+
+elsa_status elsa_layer_norm_backward(const void* dy, const void* s, const float* stats, const void* gain, const void* ds, int rows, int dim,
+                                     elsa_dtype dtype, void* dx, void* dgain, void* dbias, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!dy || !s || !stats || !gain) return fail(ELSA_ERR_NULL, "dy, s, stats and gain must not be NULL");
+    if (!dx && !dgain && !dbias) return fail(ELSA_ERR_NULL, "one of dx, dgain and dbias must be given");
+    if (dtype != ELSA_F16 && dtype != ELSA_BF16) return fail(ELSA_ERR_DTYPE, "dtype %d is neither ELSA_F16 nor ELSA_BF16", (int)dtype);
+    if (rows <= 0 || dim <= 0) return fail(ELSA_ERR_SHAPE, "non-positive dimension (rows=%d, dim=%d)", rows, dim);
+    if (dim % 8 != 0) return fail(ELSA_ERR_ALIGN, "dim=%d must be a multiple of 8 (16-byte row pitch)", dim);
+    if (!layer_norm_columns_suits(dim)) return fail(ELSA_ERR_SHAPE, "dim=%d is above 16384", dim);
+    if (!aligned16(dy) || !aligned16(s) || !aligned16(gain) || !aligned16(ds) || !aligned16(dx) || !aligned16(dgain) || !aligned16(dbias) ||
+        ((uintptr_t)stats & 7u))
+        return fail(ELSA_ERR_ALIGN, "dy, s, gain, ds, dx, dgain and dbias must be 16-byte aligned, stats 8-byte aligned");
+    if (dgain || dbias) {
+        const size_t need = layer_norm_backward_workspace(rows, dim);
+        if (!workspace || workspace_bytes < need)
+            return fail(ELSA_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace ? workspace_bytes : (size_t)0);
+        if (((uintptr_t)workspace & 255u) != 0) return fail(ELSA_ERR_ALIGN, "workspace must be 256-byte aligned");
+    }
+    return launch_layer_norm_backward((const uint16_t*)dy, (const uint16_t*)s, stats, (const uint16_t*)gain, (const uint16_t*)ds, rows, dim, dtype,
+                                      (uint16_t*)dx, (uint16_t*)dgain, (uint16_t*)dbias, (float*)workspace, (cudaStream_t)stream);
+}
+
+elsa_status elsa_rotary(const void* x, long long x_pitch, const int32_t* positions, const elsa_rotary_plan* plan, int rows, int heads,
+                        int inverse, elsa_dtype dtype, void* y, long long y_pitch, void* stream)
+{
+    if (!x || !positions || !plan || !y) return fail(ELSA_ERR_NULL, "x, positions, plan and y must not be NULL");
+    if (dtype != ELSA_F16 && dtype != ELSA_BF16) return fail(ELSA_ERR_DTYPE, "dtype %d is neither ELSA_F16 nor ELSA_BF16", (int)dtype);
+    if (plan->head_dim < 16 || plan->head_dim > 2 * ELSA_ROTARY_MAX_PAIRS || plan->head_dim % 16 != 0 || plan->axes < 1 ||
+        plan->axes > ELSA_ROTARY_MAX_AXES)
+        return fail(ELSA_ERR_SHAPE, "the plan is none that elsa_rotary_make_plan makes (head_dim=%d, axes=%d)", plan->head_dim, plan->axes);
+    if (rows <= 0 || heads <= 0) return fail(ELSA_ERR_SHAPE, "non-positive dimension (rows=%d, heads=%d)", rows, heads);
+    const long long width = (long long)heads * plan->head_dim;
+    if (x_pitch < width || y_pitch < width)
+        return fail(ELSA_ERR_SHAPE, "x_pitch=%lld and y_pitch=%lld must be at least %d heads * %d", x_pitch, y_pitch, heads, plan->head_dim);
+    if (x_pitch % 8 != 0 || y_pitch % 8 != 0) return fail(ELSA_ERR_ALIGN, "x_pitch=%lld and y_pitch=%lld must be multiples of 8", x_pitch, y_pitch);
+    if (x == y && x_pitch != y_pitch) return fail(ELSA_ERR_SHAPE, "in place x_pitch=%lld and y_pitch=%lld must be equal", x_pitch, y_pitch);
+    if (!aligned16(x) || !aligned16(y) || ((uintptr_t)positions & 3u))
+        return fail(ELSA_ERR_ALIGN, "x and y must be 16-byte aligned, positions 4-byte aligned");
+    return launch_rotary((const uint16_t*)x, x_pitch, positions, *plan, rows, heads, inverse != 0, dtype, (uint16_t*)y, y_pitch, (cudaStream_t)stream);
+}
+
+size_t elsa_packed_plan_bytes(int rows, int sequences) { return rows <= 0 || sequences <= 0 ? 0 : packed_plan_bytes(rows, sequences); }
+
+elsa_status elsa_packed_plan(const int32_t* offsets, int sequences, int rows, void* plan, size_t plan_bytes, uint32_t* dev_status, void* stream)
+{
+    if (!offsets || !plan) return fail(ELSA_ERR_NULL, "offsets and plan must not be NULL");
+    if (sequences <= 0 || rows <= 0) return fail(ELSA_ERR_SHAPE, "non-positive dimension (sequences=%d, rows=%d)", sequences, rows);
+    if (((uintptr_t)offsets & 3u) || !aligned16(plan)) return fail(ELSA_ERR_ALIGN, "offsets must be 4-byte aligned, plan 16-byte aligned");
+    const size_t need = packed_plan_bytes(rows, sequences);
+    if (plan_bytes < need) return fail(ELSA_ERR_WORKSPACE, "plan of %zu bytes needed, %zu given", need, plan_bytes);
+    return launch_packed_plan(offsets, sequences, rows, (int*)plan, dev_status, (cudaStream_t)stream);
+}
+
+namespace {
+elsa_status check_heads(const char* name, const void* t, long long pitch, long long width)
+{
+    if (!t) return fail(ELSA_ERR_NULL, "%s must not be NULL", name);
+    if (pitch < width) return fail(ELSA_ERR_SHAPE, "%s: a pitch of %lld is below the row's %lld values", name, pitch, width);
+    if (pitch % 8 != 0 || !aligned16(t)) return fail(ELSA_ERR_ALIGN, "%s must be 16-byte aligned, its pitch %lld a multiple of 8", name, pitch);
+    return ELSA_OK;
+}
+elsa_status check_packed(const elsa_packed_qkv* in, int dtype, const void* plan, int sequences)
+{
+    if (!in || !plan) return fail(ELSA_ERR_NULL, "in and plan must not be NULL");
+    if (dtype != ELSA_F16 && dtype != ELSA_BF16) return fail(ELSA_ERR_DTYPE, "dtype %d is neither ELSA_F16 nor ELSA_BF16", dtype);
+    if (in->rows <= 0 || in->heads <= 0 || in->kv_heads <= 0 || sequences <= 0)
+        return fail(ELSA_ERR_SHAPE, "non-positive dimension (rows=%d, heads=%d, kv_heads=%d, sequences=%d)", in->rows, in->heads, in->kv_heads, sequences);
+    if (in->head_dim != 32 && in->head_dim != 64 && in->head_dim != 128) return fail(ELSA_ERR_SHAPE, "head_dim=%d is neither 32, 64 nor 128", in->head_dim);
+    if (in->heads % in->kv_heads != 0) return fail(ELSA_ERR_SHAPE, "heads=%d is not a multiple of kv_heads=%d", in->heads, in->kv_heads);
+    if ((long long)in->heads * in->head_dim > 0x7fffffffLL) return fail(ELSA_ERR_SHAPE, "heads * head_dim does not fit an int");
+    if (!(in->scale - in->scale == 0.f)) return fail(ELSA_ERR_SHAPE, "scale is not finite");
+    if (!aligned16(plan)) return fail(ELSA_ERR_ALIGN, "plan must be 16-byte aligned");
+    const long long wide = (long long)in->heads * in->head_dim, narrow = (long long)in->kv_heads * in->head_dim;
+    elsa_status st = check_heads("q", in->q, in->q_pitch, wide);
+    if (st == ELSA_OK) st = check_heads("k", in->k, in->k_pitch, narrow);
+    if (st == ELSA_OK) st = check_heads("v", in->v, in->v_pitch, narrow);
+    return st;
+}
+}  // namespace
+
+elsa_status elsa_packed_attention(const elsa_packed_qkv* in, elsa_dtype dtype, const void* plan, int sequences, void* a, long long a_pitch,
+                                  float* lse, uint32_t* dev_status, void* stream)
+{
+    elsa_status st = check_packed(in, dtype, plan, sequences);
+    if (st == ELSA_OK) st = check_heads("a", a, a_pitch, (long long)in->heads * in->head_dim);
+    if (st != ELSA_OK) return st;
+    if ((uintptr_t)lse & 3u) return fail(ELSA_ERR_ALIGN, "lse must be 4-byte aligned");
+    return launch_packed_attention(*in, dtype, (const int*)plan, sequences, (uint16_t*)a, a_pitch, lse, dev_status, (cudaStream_t)stream);
+}
+
+size_t elsa_packed_attention_workspace_bytes(int rows, int heads) { return rows <= 0 || heads <= 0 ? 0 : packed_attention_workspace(rows, heads); }
+
+elsa_status elsa_packed_attention_backward(const elsa_packed_qkv* in, elsa_dtype dtype, const void* plan, int sequences, const void* a,
+                                           long long a_pitch, const float* lse, const void* da, long long da_pitch, void* dq, long long dq_pitch,
+                                           void* dk, long long dk_pitch, void* dv, long long dv_pitch, void* workspace, size_t workspace_bytes,
+                                           uint32_t* dev_status, void* stream)
+{
+    elsa_status st = check_packed(in, dtype, plan, sequences);
+    if (st != ELSA_OK) return st;
+    const long long wide = (long long)in->heads * in->head_dim, narrow = (long long)in->kv_heads * in->head_dim;
+    if ((st = check_heads("a", a, a_pitch, wide)) != ELSA_OK || (st = check_heads("da", da, da_pitch, wide)) != ELSA_OK ||
+        (st = check_heads("dq", dq, dq_pitch, wide)) != ELSA_OK || (st = check_heads("dk", dk, dk_pitch, narrow)) != ELSA_OK ||
+        (st = check_heads("dv", dv, dv_pitch, narrow)) != ELSA_OK)
+        return st;
+    if (!lse) return fail(ELSA_ERR_NULL, "lse must not be NULL");
+    if ((uintptr_t)lse & 3u) return fail(ELSA_ERR_ALIGN, "lse must be 4-byte aligned");
+    const size_t need = packed_attention_workspace(in->rows, in->heads);
+    if (!workspace || workspace_bytes < need)
+        return fail(ELSA_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace ? workspace_bytes : (size_t)0);
+    if (((uintptr_t)workspace & 255u) != 0) return fail(ELSA_ERR_ALIGN, "workspace must be 256-byte aligned");
+    return launch_packed_attention_backward(*in, dtype, (const int*)plan, sequences, (const uint16_t*)a, a_pitch, lse, (const uint16_t*)da, da_pitch,
+                                            (uint16_t*)dq, dq_pitch, (uint16_t*)dk, dk_pitch, (uint16_t*)dv, dv_pitch, workspace, dev_status,
+                                            (cudaStream_t)stream);
+}
+
 const char* elsa_last_error(void) { return g_error; }
 
 }  // extern "C"

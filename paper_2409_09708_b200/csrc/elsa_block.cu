@@ -4,50 +4,13 @@
 // column range.  All of them are HBM-bound streaming kernels: 16-byte loads and stores, fp32 arithmetic, one
 // rounding to the 16-bit type per stored value; the row-wise ones give a row to a warp, or, for the model widths
 // (128, 192, 256, 384, 512, 768, 1024), to groups of 8 to 32 lanes that have the next rows on their way.
-#include "elsa_tc_common.cuh"
+#include "elsa_row_pack.cuh"
 
 namespace elsa {
 namespace {
 
 constexpr int kWarpsPerBlock = 8;
 constexpr int kCacheVecs = 4;   // 16-byte vectors of a row each lane keeps in registers (rows up to 1024 values)
-
-template <bool kBf16>
-__device__ __forceinline__ float2 unpack2(uint32_t u)
-{
-    if constexpr (kBf16) {
-        return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
-    } else {
-        __half2 h = *reinterpret_cast<__half2*>(&u);
-        return __half22float2(h);
-    }
-}
-
-template <bool kBf16>
-__device__ __forceinline__ uint32_t pack2_rn(float a, float b)
-{
-    if constexpr (kBf16) {
-        __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-        return *reinterpret_cast<uint32_t*>(&v);
-    } else {
-        __half2 v = __floats2half2_rn(a, b);
-        return *reinterpret_cast<uint32_t*>(&v);
-    }
-}
-
-template <bool kBf16>
-__device__ __forceinline__ void unpack8(const uint4& u, float (&f)[8])
-{
-    const float2 a = unpack2<kBf16>(u.x), b = unpack2<kBf16>(u.y), c = unpack2<kBf16>(u.z), d = unpack2<kBf16>(u.w);
-    f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y; f[4] = c.x; f[5] = c.y; f[6] = d.x; f[7] = d.y;
-}
-
-template <bool kBf16>
-__device__ __forceinline__ uint4 pack8(const float (&f)[8])
-{
-    return make_uint4(pack2_rn<kBf16>(f[0], f[1]), pack2_rn<kBf16>(f[2], f[3]), pack2_rn<kBf16>(f[4], f[5]),
-                      pack2_rn<kBf16>(f[6], f[7]));
-}
 
 __device__ __forceinline__ float warp_sum(float v)
 {
@@ -89,11 +52,12 @@ __device__ __forceinline__ int window_row(const RowMapDev& m, int row)
 // grid's order); map.on_output: Yn's row r is written at window_row(r).  kAdd: the row is S = round16(A + R), written to S (which may be A's or R's own buffer:
 // each lane reads its vectors of a row before it writes them).  The statistics are those of the stored 16-bit
 // row (for kAdd: of S as rounded), mean first, then the biased variance about it; eps sits inside the root.
-// Yn = round16((s - mean) / sqrt(var + eps) * gain + beta), or no normalised output when Yn is NULL.
+// Yn = round16((s - mean) / sqrt(var + eps) * gain + beta), or no normalised output when Yn is NULL; stats (or NULL): the row's
+// mean and 1 / sqrt(var + eps).
 template <bool kBf16, bool kAdd>
 __global__ void __launch_bounds__(kWarpsPerBlock * 32)
 layer_norm_kernel(const uint16_t* A, const uint16_t* R, uint16_t* S, const uint16_t* __restrict__ gain,
-                  const uint16_t* __restrict__ beta, uint16_t* Yn, int rows, int dim, float eps, const RowMapDev map)
+                  const uint16_t* __restrict__ beta, uint16_t* Yn, float2* stats, int rows, int dim, float eps, const RowMapDev map)
 {
     pdl_wait_for_predecessors();
     pdl_release_successors();
@@ -160,6 +124,7 @@ layer_norm_kernel(const uint16_t* A, const uint16_t* R, uint16_t* S, const uint1
             for (int e = 0; e < 8; ++e) sq += (f[e] - mean) * (f[e] - mean);
         }
         const float rstd = 1.0f / sqrtf(warp_sum(sq) * inv_dim + eps);
+        if (stats != nullptr && lane == 0) stats[row] = make_float2(mean, rstd);
         uint4* y4 = reinterpret_cast<uint4*>(Yn + (size_t)(map.on_output ? mapped : row) * (size_t)dim);
         auto emit = [&](int v, const uint4& u) {
             float f[8], g[8], b[8];
@@ -188,7 +153,7 @@ layer_norm_kernel(const uint16_t* A, const uint16_t* R, uint16_t* S, const uint1
 template <bool kBf16, bool kAdd, int kLanes, int kVpl, int kUnroll, int kBlocks>
 __global__ void __launch_bounds__(kWarpsPerBlock * 32, kBlocks)
 layer_norm_rows_kernel(const uint16_t* A, const uint16_t* R, uint16_t* S, const uint16_t* __restrict__ gain,
-                       const uint16_t* __restrict__ beta, uint16_t* Yn, int rows, float eps, const RowMapDev map)
+                       const uint16_t* __restrict__ beta, uint16_t* Yn, float2* stats, int rows, float eps, const RowMapDev map)
 {
     constexpr int kGroups = 32 / kLanes;               // rows side by side in a warp
     constexpr int kRowsPerStep = kGroups * kUnroll;
@@ -247,16 +212,16 @@ layer_norm_rows_kernel(const uint16_t* A, const uint16_t* R, uint16_t* S, const 
                     const uint32_t b[4] = {w[u][c].x, w[u][c].y, w[u][c].z, w[u][c].w};
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        const float2 av = unpack2<kBf16>(a[q]), bv = unpack2<kBf16>(b[q]);
+                        const float2 av = raw2_to_float2<kBf16>(a[q]), bv = raw2_to_float2<kBf16>(b[q]);
                         const float2 t = f32x2_split(f32x2_add(f32x2(av.x, av.y), f32x2(bv.x, bv.y)));
-                        a[q] = pack2_rn<kBf16>(t.x, t.y);
+                        a[q] = pack2<kBf16>(t.x, t.y);
                     }
                     if (r < rows) reinterpret_cast<uint4*>(S + (size_t)r * (size_t)kDim)[sub + kLanes * c] = make_uint4(a[0], a[1], a[2], a[3]);
                 }
                 // the statistics are those of the row as stored
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const float2 v = unpack2<kBf16>(a[q]);
+                    const float2 v = raw2_to_float2<kBf16>(a[q]);
                     f[u][c][q] = f32x2(v.x, v.y);
                 }
             }
@@ -284,6 +249,7 @@ layer_norm_rows_kernel(const uint16_t* A, const uint16_t* R, uint16_t* S, const 
             }
             const float2 t = f32x2_split(sq2);
             rstd[u] = 1.0f / sqrtf(group_sum(t.x + t.y) * inv_dim + eps);
+            if (stats != nullptr && sub == 0 && row_of(step, u) < rows) stats[row_of(step, u)] = make_float2(mean[u], rstd[u]);
         }
         // gain and bias from the first-level cache: in registers they would cost a resident block or two
 #pragma unroll
@@ -294,7 +260,7 @@ layer_norm_rows_kernel(const uint16_t* A, const uint16_t* R, uint16_t* S, const 
             uint64_t g2[4], b2[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const float2 gv = unpack2<kBf16>(g[q]), bv = unpack2<kBf16>(b[q]);
+                const float2 gv = raw2_to_float2<kBf16>(g[q]), bv = raw2_to_float2<kBf16>(b[q]);
                 g2[q] = f32x2(gv.x, gv.y);
                 b2[q] = f32x2(bv.x, bv.y);
             }
@@ -305,7 +271,7 @@ layer_norm_rows_kernel(const uint16_t* A, const uint16_t* R, uint16_t* S, const 
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const float2 t = f32x2_split(f32x2_fma(f32x2_mul(f[u][c][q], rstd2), g2[q], b2[q]));
-                    o[q] = pack2_rn<kBf16>(t.x, t.y);
+                    o[q] = pack2<kBf16>(t.x, t.y);
                 }
                 if (out_row[u] >= 0)
                     reinterpret_cast<uint4*>(Yn + (size_t)out_row[u] * (size_t)kDim)[sub + kLanes * c] = make_uint4(o[0], o[1], o[2], o[3]);
@@ -362,10 +328,16 @@ unsigned streaming_grid(long long work_items, int per_block, const DeviceInfo& d
 
 }  // namespace
 
+bool layer_norm_rows_suits(int dim)
+{
+    return dim == 128 || dim == 192 || dim == 256 || dim == 384 || dim == 512 || dim == 768 || dim == 1024;
+}
+
 elsa_status launch_layer_norm(const uint16_t* A, const uint16_t* R, uint16_t* S, const uint16_t* gain,
                               const uint16_t* beta, uint16_t* Yn, int rows, int dim, float eps, elsa_dtype dtype,
-                              cudaStream_t stream, const RowMap* row_map)
+                              cudaStream_t stream, const RowMap* row_map, float* stats)
 {
+    float2* stats2 = reinterpret_cast<float2*>(stats);
     RowMapDev map = {};
     if (row_map != nullptr && row_map->H != 0) {
         const RowMap& r = *row_map;
@@ -392,7 +364,7 @@ elsa_status launch_layer_norm(const uint16_t* A, const uint16_t* R, uint16_t* S,
         const int steps = (rows - 1) / ((32 / LANES) * UNROLL) + 1, resident = dev.sm_count * BLOCKS;                     \
         const int blocks = (steps + kWarpsPerBlock - 1) / kWarpsPerBlock, most = blocks >= 8 * resident ? 4 * resident : resident; \
         launch_pdl(layer_norm_rows_kernel<BF, ADD, LANES, VPL, UNROLL, BLOCKS>, dim3((unsigned)(blocks < most ? blocks : most)), block, 0, \
-                   stream, 1, A, R, S, gain, beta, Yn, rows, eps, map);                                                   \
+                   stream, 1, A, R, S, gain, beta, Yn, stats2, rows, eps, map);                                                   \
     } while (0)
 #define ELSA_LN_ROWS(LANES, VPL, UNROLL, BLOCKS, UNROLL_ADD, BLOCKS_ADD)                                                  \
     do {                                                                                                                  \
@@ -417,11 +389,11 @@ elsa_status launch_layer_norm(const uint16_t* A, const uint16_t* R, uint16_t* S,
 #undef ELSA_LN_ROWS
     const unsigned grid = streaming_grid(rows, kWarpsPerBlock, dev);
     if (dtype == ELSA_BF16) {
-        if (add) launch_pdl(layer_norm_kernel<true, true>, dim3(grid), block, 0, stream, 1, A, R, S, gain, beta, Yn, rows, dim, eps, map);
-        else launch_pdl(layer_norm_kernel<true, false>, dim3(grid), block, 0, stream, 1, A, R, S, gain, beta, Yn, rows, dim, eps, map);
+        if (add) launch_pdl(layer_norm_kernel<true, true>, dim3(grid), block, 0, stream, 1, A, R, S, gain, beta, Yn, stats2, rows, dim, eps, map);
+        else launch_pdl(layer_norm_kernel<true, false>, dim3(grid), block, 0, stream, 1, A, R, S, gain, beta, Yn, stats2, rows, dim, eps, map);
     } else {
-        if (add) launch_pdl(layer_norm_kernel<false, true>, dim3(grid), block, 0, stream, 1, A, R, S, gain, beta, Yn, rows, dim, eps, map);
-        else launch_pdl(layer_norm_kernel<false, false>, dim3(grid), block, 0, stream, 1, A, R, S, gain, beta, Yn, rows, dim, eps, map);
+        if (add) launch_pdl(layer_norm_kernel<false, true>, dim3(grid), block, 0, stream, 1, A, R, S, gain, beta, Yn, stats2, rows, dim, eps, map);
+        else launch_pdl(layer_norm_kernel<false, false>, dim3(grid), block, 0, stream, 1, A, R, S, gain, beta, Yn, stats2, rows, dim, eps, map);
     }
     return launched(add ? "residual_add_layer_norm" : "layer_norm");
 }

@@ -220,7 +220,21 @@ struct RowMap {
 };
 elsa_status launch_layer_norm(const uint16_t* A, const uint16_t* R, uint16_t* S, const uint16_t* gain,
                               const uint16_t* beta, uint16_t* Yn, int rows, int dim, float eps, elsa_dtype dtype,
-                              cudaStream_t stream, const RowMap* row_map = nullptr);
+                              cudaStream_t stream, const RowMap* row_map = nullptr, float* stats = nullptr);
+// Whether launch_layer_norm has a form of its own for rows of this width (stats: mean and 1 / sqrt(var + eps) of each row, or NULL).
+bool layer_norm_rows_suits(int dim);
+// The same without a row map for any width up to 16384, and the gradient: dX = dS (or nothing) + the gradient at S, dgain and dbias
+// (each of the three may be NULL) through layer_norm_backward_workspace bytes of partial sums.
+bool layer_norm_columns_suits(int dim);
+elsa_status launch_layer_norm_columns(const uint16_t* A, const uint16_t* R, uint16_t* S, const uint16_t* gain, const uint16_t* beta,
+                                      uint16_t* Y, float* stats, int rows, int dim, float eps, elsa_dtype dtype, cudaStream_t stream);
+size_t layer_norm_backward_workspace(int rows, int dim);
+elsa_status launch_layer_norm_backward(const uint16_t* dY, const uint16_t* S, const float* stats, const uint16_t* gain, const uint16_t* dS,
+                                       int rows, int dim, elsa_dtype dtype, uint16_t* dX, uint16_t* dgain, uint16_t* dbias, float* partial,
+                                       cudaStream_t stream);
+// y[r][h] = x[r][h] turned by the angles of row r's positions, for `heads` adjacent heads; pitches in values.
+elsa_status launch_rotary(const uint16_t* x, long long x_pitch, const int32_t* positions, const elsa_rotary_plan& plan, int rows, int heads,
+                          bool inverse, elsa_dtype dtype, uint16_t* y, long long y_pitch, cudaStream_t stream);
 // Y = act(Y) over `count` values (count % 8 == 0); act as in the GEMM epilogues.
 elsa_status launch_act_inplace(uint16_t* Y, long long count, int act, elsa_dtype dtype, cudaStream_t stream);
 // dst[r][0 .. cols) = src[r][col0 .. col0 + cols); src rows of src_ld values; all multiples of 8.
@@ -244,6 +258,16 @@ bool window_attention_suits(int tokens, int heads, int dim);
 elsa_status launch_window_attention(const uint16_t* qkv, int windows, int tokens, int heads, int dim, elsa_dtype dtype, uint16_t* out,
                                     uint32_t* dev_status, cudaStream_t stream, const float* bias, const float* mask, int n_masks,
                                     int bias_pitch, const DeviceInfo& dev);
+// Attention over packed sequences: the plan from the offsets, the forward call and the gradient (arguments as checked by the ABI).
+size_t packed_plan_bytes(int rows, int sequences);
+elsa_status launch_packed_plan(const int32_t* offsets, int sequences, int rows, int* plan, uint32_t* dev_status, cudaStream_t stream);
+elsa_status launch_packed_attention(const elsa_packed_qkv& in, elsa_dtype dtype, const int* plan, int sequences, uint16_t* a, long long a_pitch,
+                                    float* lse, uint32_t* dev_status, cudaStream_t stream);
+size_t packed_attention_workspace(int rows, int heads);
+elsa_status launch_packed_attention_backward(const elsa_packed_qkv& in, elsa_dtype dtype, const int* plan, int sequences, const uint16_t* a,
+                                             long long a_pitch, const float* lse, const uint16_t* da, long long da_pitch, uint16_t* dq,
+                                             long long dq_pitch, uint16_t* dk, long long dk_pitch, uint16_t* dv, long long dv_pitch,
+                                             void* workspace, uint32_t* dev_status, cudaStream_t stream);
 // Operand forms of the backward pass.  transpose_packed: dst [in][out] (out a multiple of 8) = the transposed masked weight,
 // positions that were not kept zero.  colsum: db [C] = column sums of src [R][C], through ceil(R / 512) * C floats of scratch.
 elsa_status launch_transpose_packed(const uint16_t* vals, const uint32_t* idx, uint16_t* dst, int out, int in, int N, int M, cudaStream_t stream);

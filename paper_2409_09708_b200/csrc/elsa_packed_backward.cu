@@ -1,0 +1,409 @@
+// Gradient of the attention over packed sequences.  With p_ij = exp(scale q_i . k_j - lse_i), recomputed from the forward's lse, and
+// delta_i = da_i . a_i:
+//     ds_ij = p_ij (da_i . v_j - delta_i)
+//     dq_i = scale sum_j ds_ij k_j        dk_j = scale sum_i ds_ij q_i        dv_j = sum_i p_ij da_i
+// dk and dv also sum over the query heads that share the key head.  Two kernels of one form, because the two directions of the sum
+// keep different rows: the first keeps 128 query rows of a head and walks the keys (dq, and delta on the way), the second keeps
+// 128 key rows of a key head and walks the queries of all its heads (dk, dv).  That is seven products where one kernel would do with
+// five, but no sum leaves the SM unfinished: no atomics, no partial sums in memory, the same bits every time.
+//
+// Per tile of 64 walked rows (X1, X2 kept; Y1, Y2 walked):      dq kernel        dk, dv kernel
+//     S  = X1 Y1^T   (128 x 64 scores)                           q k^T            k q^T
+//     T  = X2 Y2^T                                               da v^T           v da^T
+//     acc2 += ds Y1  (ds rounded to the 16-bit type)             ds k             ds^T q
+//     acc1 += p Y2   (p rounded to the 16-bit type)              -                p^T da
+// All products run on tcgen05; S and T go to fp32 columns of tensor memory, p and ds come back over them as A operands.  Two stages of
+// S and T, each with its own four warps (a row a lane): one stage's exponentials run under the other's products.
+// In the second kernel lse and delta belong to the walked rows: they come with each tile into shared memory.
+// What bounds it: per tile 512 cycles of exponentials, and products of 640 (384) cycles for heads of 64 columns, 1280 (1024) for 128:
+// the shared memory's 128 bytes a cycle bound S and T (6 KB for each 16 columns of the head, 48 cycles against the tensor core's 32).
+#include <atomic>
+
+#include "elsa_packed.cuh"
+
+namespace elsa {
+namespace {
+
+constexpr int kWalk = 64;                // walked rows of a tile
+constexpr int kRing = 4;                 // tiles of them on their way
+
+template <int kD>
+struct BackwardShape {
+    static constexpr int kThreads = 2 * 128 + 64;
+    static constexpr int kKeptBytes = TileShape<kD>::bytes(128), kWalkBytes = TileShape<kD>::bytes(kWalk);
+    static constexpr int kAcc1 = 256, kAcc2 = 256 + kD;              // tensor-memory columns; stage g: S at 128 g, T at 128 g + 64
+    static constexpr int kVectorBytes = 2 * kWalk * 4;               // -lse log2(e), delta
+    static constexpr int kSmemBytes = 2 * kKeptBytes + kRing * (2 * kWalkBytes + kVectorBytes) + 1024 /* delta of the kept rows */ +
+                                      1024 /* alignment */ + 256 /* barriers */;
+};
+
+struct BackwardParams {
+    CUtensorMap map_x1, map_x2;          // boxes of 128 rows
+    CUtensorMap map_y1, map_y2;          // boxes of 64 rows
+    const int* plan;
+    const uint16_t* a;                   // dq kernel: for delta
+    const uint16_t* da;
+    const float* lse;                    // [heads][rows]
+    float* minus_lse;                    // [heads][rows]: -lse log2(e), made by the dq kernel for the other
+    float* delta;                        // [heads][rows]
+    uint16_t* out1;                      // dv
+    uint16_t* out2;                      // dq or dk
+    long long a_pitch, da_pitch, out1_pitch, out2_pitch;
+    int rows, sequences, heads, kv_heads, group;
+    int causal;
+    float scale, scale_log2;
+    uint32_t idesc_s, idesc_acc;
+    uint32_t* dev_status;
+};
+
+// Four bytes global -> shared, zero where `in` is false; without a register in between.
+__device__ __forceinline__ void copy_word(uint32_t dst, const float* src, bool in)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(in ? 4 : 0) : "memory");
+}
+// One arrival of this thread on the barrier once its copies so far have landed.
+__device__ __forceinline__ void copies_arrive(uint32_t bar)
+{
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+template <bool kBf16, int kD, bool kKeys>
+__global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attention_backward_kernel(const __grid_constant__ BackwardParams p)
+{
+    using B = BackwardShape<kD>;
+    pdl_wait_for_predecessors();
+    pdl_release_successors();
+    const int kept_heads = kKeys ? p.kv_heads : p.heads;
+    const int head = blockIdx.x % kept_heads;
+    PackedTile tile;
+    // under a causal mask the last query tiles and the first key tiles have the most to do
+    if (!plan_tile<128>(p.plan, p.rows, p.sequences, blockIdx.x / kept_heads, p.causal != 0 && !kKeys, p.dev_status, tile)) return;
+
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t x1_smem = smem_base, x2_smem = smem_base + B::kKeptBytes;
+    auto y1_smem = [&](int s) { return smem_base + (uint32_t)(2 * B::kKeptBytes + 2 * s * B::kWalkBytes); };
+    auto y2_smem = [&](int s) { return y1_smem(s) + (uint32_t)B::kWalkBytes; };
+    const uint32_t vectors = smem_base + (uint32_t)(2 * B::kKeptBytes + 2 * kRing * B::kWalkBytes);
+    const uint32_t kept_delta = vectors + kRing * B::kVectorBytes;                     // [2][128] floats
+    const uint32_t bars = kept_delta + 1024;
+    enum { kXFull = 0, kYFull = 1, kYEmpty = 1 + kRing, kSFull = 1 + 2 * kRing, kPFull = 3 + 2 * kRing, kDone = 5 + 2 * kRing, kBars };
+    auto bar = [&](int which, int i) { return bars + (uint32_t)(8 * (which + i)); };
+    const uint32_t tmem_holder_addr = bars + 8 * kBars;
+    uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(smem_raw + (tmem_holder_addr - smem_u32(smem_raw)));
+    volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem_raw + (tmem_holder_addr + 8 - smem_u32(smem_raw)));
+    static_assert(8 * kBars + 16 <= 256, "barriers");
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr int kTmaWarp = 8, kMmaWarp = 9;
+    // walked tiles: keys from the sequence's start (causal: up to the last kept row); queries to its end (causal: from the first kept row)
+    const int walk_from = kKeys && p.causal ? tile.first / kWalk : 0;
+    const int walk_end = !kKeys && p.causal && tile.first + 128 < tile.len ? tile.first + 128 : tile.len;
+    const int per_head = (walk_end - 1) / kWalk + 1 - walk_from;
+    const int n = kKeys ? per_head * p.group : per_head;
+    if (warp == kMmaWarp) {
+        if (lane == 0) {
+            mbar_init(bar(kXFull, 0), 1);
+            for (int s = 0; s < kRing; ++s) {
+                mbar_init(bar(kYFull, s), kKeys ? 33 : 1);
+                mbar_init(bar(kYEmpty, s), 1);
+            }
+            for (int g = 0; g < 2; ++g) {
+                mbar_init(bar(kSFull, g), 1);
+                mbar_init(bar(kPFull, g), 4);
+            }
+            mbar_init(bar(kDone, 0), 1);
+            *abort_flag = 0;
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        __syncwarp();
+        tmem_alloc(tmem_holder_addr, 512);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_holder;
+
+    bool ok = true;
+    auto wait = [&](uint32_t b, int count, uint32_t site) {          // for the count-th completion of a barrier, from 0
+        ok = mbar_wait(b, (uint32_t)(count & 1), abort_flag, p.dev_status, site);
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        return ok;
+    };
+    if (warp == kTmaWarp) {
+        // ------------------------------------------------ TMA producer
+        const bool elected = elect_one();
+        if (elected) {
+            mbar_arrive_expect_tx(bar(kXFull, 0), 2 * B::kKeptBytes);
+            load_tile<kD, 128>(x1_smem, &p.map_x1, bar(kXFull, 0), head * kD, tile.begin + tile.first);
+            load_tile<kD, 128>(x2_smem, &p.map_x2, bar(kXFull, 0), head * kD, tile.begin + tile.first);
+        }
+        __syncwarp();
+        int walk_head = kKeys ? head * p.group : head / p.group, t = 0;
+        for (int it = 0; it < n; ++it, ++t) {
+            const int s = it % kRing;
+            if (kKeys && t == per_head) { t = 0; ++walk_head; }
+            const int row = (walk_from + t) * kWalk;                 // in the sequence
+            if (it >= kRing && !wait(bar(kYEmpty, s), it / kRing - 1, 80)) break;
+            if (elected) {
+                mbar_arrive_expect_tx(bar(kYFull, s), 2 * B::kWalkBytes);
+                load_tile<kD, kWalk>(y1_smem(s), &p.map_y1, bar(kYFull, s), walk_head * kD, tile.begin + row);
+                load_tile<kD, kWalk>(y2_smem(s), &p.map_y2, bar(kYFull, s), walk_head * kD, tile.begin + row);
+            }
+            __syncwarp();
+            if constexpr (kKeys) {
+                const size_t at = (size_t)walk_head * (size_t)p.rows + (size_t)(tile.begin + row);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int c = lane + 32 * h;
+                    const bool in = row + c < tile.len;
+                    const uint32_t dst = vectors + (uint32_t)(s * B::kVectorBytes + 4 * c);
+                    copy_word(dst, p.minus_lse + (in ? at + c : 0), in);
+                    copy_word(dst + 4 * kWalk, p.delta + (in ? at + c : 0), in);
+                }
+                copies_arrive(bar(kYFull, s));
+            }
+        }
+    } else if (warp == kMmaWarp) {
+        // ------------------------------------------------ MMA issuer: S and T of tile it, then the sums of tile it - 1
+        const uint32_t elected = elect_one() ? 1u : 0u;
+        const uint32_t tmem_u = __reduce_or_sync(0xFFFFFFFFu, tmem_base);
+        wait(bar(kXFull, 0), 0, 81);
+        for (int it = 0; ok && it <= n; ++it) {
+            if (it < n) {
+                const int s = it % kRing, g = it & 1;
+                if (!wait(bar(kYFull, s), it / kRing, 82)) break;
+                const int left = tile.len - (walk_from + it % per_head) * kWalk;
+                if (left < kWalk && (left & 15) != 0) {
+                    zero_rows<kD, kWalk>(y1_smem(s), left, (left + 15) & ~15, lane);
+                    zero_rows<kD, kWalk>(y2_smem(s), left, (left + 15) & ~15, lane);
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                }
+                tc_fence_after();
+                const uint32_t t_s = tmem_u + (uint32_t)(128 * g);
+#pragma unroll
+                for (int k = 0; k < kD / 16; ++k)
+                    umma_f16_if(t_s, desc_k_major<kD, 128>(x1_smem, k), desc_k_major<kD, kWalk>(y1_smem(s), k), p.idesc_s, (uint32_t)(k != 0), elected);
+#pragma unroll
+                for (int k = 0; k < kD / 16; ++k)
+                    umma_f16_if(t_s + 64, desc_k_major<kD, 128>(x2_smem, k), desc_k_major<kD, kWalk>(y2_smem(s), k), p.idesc_s, (uint32_t)(k != 0), elected);
+                umma_commit_if(bar(kSFull, g), elected);
+            }
+            if (it > 0) {
+                const int m = it - 1, s = m % kRing, g = m & 1;
+                if (!wait(bar(kPFull, g), m >> 1, 83)) break;
+                tc_fence_after();
+                const int left = tile.len - (walk_from + m % per_head) * kWalk;
+                const int steps = left >= kWalk ? kWalk / 16 : (left + 15) / 16;
+                const uint32_t t_s = tmem_u + (uint32_t)(128 * g);
+                if constexpr (kKeys) {
+                    for (int k = 0; k < steps; ++k)
+                        umma_f16_ts_if(tmem_u + B::kAcc1, t_s + (uint32_t)(8 * k), desc_mn_major<kD, kWalk>(y2_smem(s), k), p.idesc_acc, (uint32_t)(m != 0 || k != 0), elected);
+                }
+                for (int k = 0; k < steps; ++k)
+                    umma_f16_ts_if(tmem_u + B::kAcc2, t_s + (uint32_t)(64 + 8 * k), desc_mn_major<kD, kWalk>(y1_smem(s), k), p.idesc_acc, (uint32_t)(m != 0 || k != 0), elected);
+                umma_commit_if(bar(kYEmpty, s), elected);
+                if (m == n - 1) umma_commit_if(bar(kDone, 0), elected);
+            }
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------ p and ds, then the sums' way out: group g takes the tiles g, g + 2, ...
+        const int g = warp >> 2, quarter = warp & 3;
+        const int row0 = tile.first + 32 * quarter, row = row0 + lane;                 // kept row, in the sequence
+        const bool exists = row < tile.len;
+        const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16);
+        float minus_lse = 0.f, delta = 0.f;
+        if constexpr (!kKeys) {
+            // delta: half a row by each group
+            const size_t at = (size_t)head * (size_t)p.rows + (size_t)(tile.begin + row);
+            float part = 0.f;
+            if (exists) {
+                const uint4* a4 = reinterpret_cast<const uint4*>(p.a + (long long)(tile.begin + row) * p.a_pitch + head * kD + g * (kD / 2));
+                const uint4* d4 = reinterpret_cast<const uint4*>(p.da + (long long)(tile.begin + row) * p.da_pitch + head * kD + g * (kD / 2));
+#pragma unroll
+                for (int v = 0; v < kD / 16; ++v) {
+                    const uint4 x = __ldg(a4 + v), y = __ldg(d4 + v);
+                    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float2 u = raw2_to_float2<kBf16>(xs[e]), w = raw2_to_float2<kBf16>(ys[e]);
+                        part = fmaf(u.x, w.x, fmaf(u.y, w.y, part));
+                    }
+                }
+                minus_lse = -1.4426950408889634f * __ldg(p.lse + at);
+            }
+            const uint32_t mine = kept_delta + (uint32_t)(4 * (quarter * 32 + lane));
+            asm volatile("st.shared.f32 [%0], %1;" ::"r"(mine + (uint32_t)(512 * g)), "f"(part) : "memory");
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            float first, second;
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(first) : "r"(mine) : "memory");
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(second) : "r"(mine + 512u) : "memory");
+            delta = first + second;
+            if (g == 0 && exists) {
+                p.minus_lse[at] = minus_lse;
+                p.delta[at] = delta;
+            }
+        }
+        const uint64_t scale2 = f32x2(p.scale_log2, p.scale_log2);
+        for (int it = g; it < n; it += 2) {
+            const int s = it % kRing;
+            const int walked = (walk_from + it % per_head) * kWalk;                    // first walked row, in the sequence
+            if constexpr (kKeys) {
+                if (!wait(bar(kYFull, s), it / kRing, 84)) break;                      // lse and delta
+            }
+            if (!wait(bar(kSFull, g), it >> 1, 85)) break;
+            tc_fence_after();
+            if (row0 < tile.len) {
+                // columns [lo, hi) take part.  Walked queries behind the sequence's end need no test: their rows of q and da are zero,
+                // and so are lse and delta, so that p = 1 meets zeros and ds = 0.
+                const int lo = kKeys && p.causal ? row - walked : 0;
+                const int hi = kKeys ? kWalk : (p.causal && row + 1 < tile.len ? row + 1 : tile.len) - walked;
+                const bool whole = __all_sync(0xFFFFFFFFu, lo <= 0 && hi >= kWalk);
+                const uint32_t vec = vectors + (uint32_t)(s * B::kVectorBytes);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    uint32_t rs[32], rt[32];
+                    tmem_ld_32x32b_x32(t_lane + (uint32_t)(128 * g + 32 * u), rs);
+                    tmem_ld_32x32b_x32(t_lane + (uint32_t)(128 * g + 64 + 32 * u), rt);
+                    tmem_wait_ld();
+                    uint32_t wp[16], wd[16];
+#pragma unroll
+                    for (int i = 0; i < 16; i += 2) {
+                        float4 l4 = make_float4(minus_lse, minus_lse, minus_lse, minus_lse), d4 = make_float4(delta, delta, delta, delta);
+                        if constexpr (kKeys) {
+                            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(l4.x), "=f"(l4.y), "=f"(l4.z), "=f"(l4.w) : "r"(vec + (uint32_t)(128 * u + 8 * i)));
+                            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(d4.x), "=f"(d4.y), "=f"(d4.z), "=f"(d4.w) : "r"(vec + (uint32_t)(4 * kWalk + 128 * u + 8 * i)));
+                        }
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const int c = 2 * (i + h);
+                            const uint64_t l2 = h == 0 ? f32x2(l4.x, l4.y) : f32x2(l4.z, l4.w);
+                            const uint64_t d2 = h == 0 ? f32x2(-d4.x, -d4.y) : f32x2(-d4.z, -d4.w);
+                            const float2 e = f32x2_split(f32x2_fma(f32x2(__uint_as_float(rs[c]), __uint_as_float(rs[c + 1])), scale2, l2));
+                            float2 pp = make_float2(exp2_approx(e.x), exp2_approx(e.y));
+                            float2 ds = f32x2_split(f32x2_mul(f32x2(pp.x, pp.y), f32x2_add(f32x2(__uint_as_float(rt[c]), __uint_as_float(rt[c + 1])), d2)));
+                            if (!whole) {
+                                const int col = 32 * u + c;
+                                if (col < lo || col >= hi) pp.x = ds.x = 0.f;
+                                if (col + 1 < lo || col + 1 >= hi) pp.y = ds.y = 0.f;
+                            }
+                            if constexpr (kKeys) wp[i + h] = pack2<kBf16>(pp.x, pp.y);
+                            wd[i + h] = pack2<kBf16>(ds.x, ds.y);
+                        }
+                    }
+                    if constexpr (kKeys) tmem_st_32x32b_x16(t_lane + (uint32_t)(128 * g + 16 * u), wp);
+                    tmem_st_32x32b_x16(t_lane + (uint32_t)(128 * g + 64 + 16 * u), wd);
+                }
+                tmem_wait_st();
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(kPFull, g));
+        }
+        if (ok && row0 < tile.len && wait(bar(kDone, 0), 0, 86)) {
+            tc_fence_after();
+            // all copies and products have ended: the ring is staging room
+            const uint32_t stage = y1_smem(0) + (uint32_t)(4096 * warp);
+            const long long first = tile.begin + row0;
+            if constexpr (kKeys) {
+                uint16_t* dst = (g == 0 ? p.out1 + first * p.out1_pitch : p.out2 + first * p.out2_pitch) + head * kD;
+                constexpr int kCols = TileShape<kD>::kCols;
+#pragma unroll
+                for (int c = 0; c < kD; c += kCols)
+                    store_rows<kBf16, kCols>(t_lane + (uint32_t)((g == 0 ? B::kAcc1 : B::kAcc2) + c), g == 0 ? 1.f : p.scale, stage, dst + c,
+                                             g == 0 ? p.out1_pitch : p.out2_pitch, tile.len - row0, lane);
+            } else {
+                // half the columns by each group; heads of 32 columns by the first alone
+                constexpr int kCols = kD == 128 ? 64 : 32;
+                if (kCols * g < kD)
+                    store_rows<kBf16, kCols>(t_lane + (uint32_t)(B::kAcc2 + kCols * g), p.scale, stage, p.out2 + first * p.out2_pitch + head * kD + kCols * g,
+                                             p.out2_pitch, tile.len - row0, lane);
+            }
+        }
+    }
+    if (!ok) let_copies_land();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == kMmaWarp) {
+        tc_fence_after();
+        tmem_dealloc(tmem_base, 512);
+    }
+}
+
+template <bool kBf16, int kD, bool kKeys>
+elsa_status launch(const BackwardParams& p, cudaStream_t stream, const DeviceInfo& dev)
+{
+    using B = BackwardShape<kD>;
+    static_assert(2 * kRing * B::kWalkBytes >= 8 * 4096, "staging room");
+    auto kernel = packed_attention_backward_kernel<kBf16, kD, kKeys>;
+    static std::atomic<bool> attr_set[64];
+    const int slot = dev.device & 63;
+    if (!attr_set[slot].load(std::memory_order_acquire)) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, B::kSmemBytes) != cudaSuccess) {
+            cudaError_t e = cudaGetLastError();
+            return fail(ELSA_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
+        }
+        attr_set[slot].store(true, std::memory_order_release);
+    }
+    const long long items = (long long)plan_capacity(p.rows, p.sequences, 128) * (kKeys ? p.kv_heads : p.heads);
+    if (items > 0x7fffffffLL) return fail(ELSA_ERR_SHAPE, "tiles * heads does not fit an int");
+    ProfileScope scope(ELSA_KERNEL_PACKED_ATTENTION_BACKWARD, stream);
+    cudaError_t e = launch_pdl(kernel, dim3((unsigned)items), dim3(B::kThreads), (size_t)B::kSmemBytes, stream, 1, p);
+    if (e != cudaSuccess) return fail(ELSA_ERR_CUDA, "packed attention backward launch: %s", cudaGetErrorString(e));
+    return launched("packed_attention_backward");
+}
+
+template <bool kBf16, int kD>
+elsa_status launch_both(const BackwardParams& queries, const BackwardParams& keys, cudaStream_t stream, const DeviceInfo& dev)
+{
+    const elsa_status st = launch<kBf16, kD, false>(queries, stream, dev);
+    return st != ELSA_OK ? st : launch<kBf16, kD, true>(keys, stream, dev);
+}
+
+}  // namespace
+
+size_t packed_attention_workspace(int rows, int heads) { return round_up((size_t)rows * (size_t)heads * sizeof(float), 256) * 2; }
+
+elsa_status launch_packed_attention_backward(const elsa_packed_qkv& in, elsa_dtype dtype, const int* plan, int sequences, const uint16_t* a,
+                                             long long a_pitch, const float* lse, const uint16_t* da, long long da_pitch, uint16_t* dq,
+                                             long long dq_pitch, uint16_t* dk, long long dk_pitch, uint16_t* dv, long long dv_pitch,
+                                             void* workspace, uint32_t* dev_status, cudaStream_t stream)
+{
+    DeviceInfo dev;
+    elsa_status st = device_info(&dev);
+    if (st != ELSA_OK) return st;
+    const int d = in.head_dim, rows = in.rows;
+    const long long wide = (long long)in.heads * d, narrow = (long long)in.kv_heads * d;
+    BackwardParams q, k;
+    q.plan = plan; q.a = a; q.da = da; q.lse = lse;
+    q.minus_lse = static_cast<float*>(workspace);
+    q.delta = reinterpret_cast<float*>(static_cast<char*>(workspace) + packed_attention_workspace(rows, in.heads) / 2);
+    q.a_pitch = a_pitch; q.da_pitch = da_pitch;
+    q.rows = rows; q.sequences = sequences; q.heads = in.heads; q.kv_heads = in.kv_heads; q.group = in.heads / in.kv_heads;
+    q.causal = in.causal ? 1 : 0;
+    q.scale = in.scale; q.scale_log2 = in.scale * 1.4426950408889634f;
+    q.idesc_s = packed_idesc(dtype, kWalk, false);
+    q.idesc_acc = packed_idesc(dtype, d, true);
+    q.dev_status = dev_status;
+    k = q;
+    q.out1 = nullptr; q.out1_pitch = 0;
+    q.out2 = dq; q.out2_pitch = dq_pitch;
+    k.out1 = dv; k.out1_pitch = dv_pitch;
+    k.out2 = dk; k.out2_pitch = dk_pitch;
+    if ((st = make_map_heads(&q.map_x1, in.q, rows, wide, in.q_pitch, d, 128, "q")) != ELSA_OK) return st;
+    if ((st = make_map_heads(&q.map_x2, da, rows, wide, da_pitch, d, 128, "da")) != ELSA_OK) return st;
+    if ((st = make_map_heads(&q.map_y1, in.k, rows, narrow, in.k_pitch, d, kWalk, "k")) != ELSA_OK) return st;
+    if ((st = make_map_heads(&q.map_y2, in.v, rows, narrow, in.v_pitch, d, kWalk, "v")) != ELSA_OK) return st;
+    if ((st = make_map_heads(&k.map_x1, in.k, rows, narrow, in.k_pitch, d, 128, "k")) != ELSA_OK) return st;
+    if ((st = make_map_heads(&k.map_x2, in.v, rows, narrow, in.v_pitch, d, 128, "v")) != ELSA_OK) return st;
+    if ((st = make_map_heads(&k.map_y1, in.q, rows, wide, in.q_pitch, d, kWalk, "q")) != ELSA_OK) return st;
+    if ((st = make_map_heads(&k.map_y2, da, rows, wide, da_pitch, d, kWalk, "da")) != ELSA_OK) return st;
+    const bool bf = dtype == ELSA_BF16;
+    if (d == 32) return bf ? launch_both<true, 32>(q, k, stream, dev) : launch_both<false, 32>(q, k, stream, dev);
+    if (d == 64) return bf ? launch_both<true, 64>(q, k, stream, dev) : launch_both<false, 64>(q, k, stream, dev);
+    return bf ? launch_both<true, 128>(q, k, stream, dev) : launch_both<false, 128>(q, k, stream, dev);
+}
+
+}  // namespace elsa
