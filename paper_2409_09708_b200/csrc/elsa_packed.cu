@@ -26,23 +26,26 @@
 namespace elsa {
 namespace {
 
-constexpr int kKeys = 128;               // keys of a tile
-constexpr int kStages = 2;
-
 template <int kD>
 struct ForwardShape {
     static constexpr int kTiles = kD > 64 ? 2 : 1;                   // tiles of 128 query rows
-    static constexpr bool kPOverS = kD > 64;
+    static constexpr int kKeys = kD > 64 ? 128 : 64;                 // keys of a tile
+    static constexpr int kChunk = kD > 64 ? 64 : 32;                 // scores of a row in registers at a time
+    static constexpr int kStages = 2;                                // of V of a tile and K of the next
     static constexpr int kThreads = kTiles * 128 + 64;
-    static constexpr int kPerSm = kD > 64 ? 1 : 2;
-    static constexpr int kTmemCols = kD > 64 ? 512 : 256;
-    static constexpr int kPCol = kPOverS ? 0 : 128, kOCol = kPOverS ? 128 : 192;
-    static constexpr int kTileBytes = TileShape<kD>::bytes(128);
-    static constexpr int kSmemBytes = (kTiles + 2 * kStages) * kTileBytes + 1024 /* alignment */ + 256 /* barriers */;
+    static constexpr int kPerSm = kD > 64 ? 1 : 4;
+    static constexpr int kTmemCols = 512 / kPerSm;
+    static constexpr int kTileCols = kTmemCols / kTiles;             // a query tile's share: its scores, then O
+    static constexpr int kOCol = kKeys;
+    static constexpr int kQBytes = TileShape<kD>::bytes(128), kKvBytes = TileShape<kD>::bytes(kKeys);
+    static constexpr int kSmemBytes = kTiles * kQBytes + 2 * kStages * kKvBytes + 1024 /* alignment */ + 256 /* barriers */;
+    static_assert(kOCol + kD <= kTileCols, "tensor memory");
+    static_assert(kStages % 2 == 0, "a tile's parity is its stage's");
 };
 
 struct ForwardParams {
-    CUtensorMap map_q, map_k, map_v;     // boxes of 128 rows
+    CUtensorMap map_q;                   // boxes of 128 rows
+    CUtensorMap map_k, map_v;            // boxes of a key tile's rows
     const int* plan;
     uint16_t* a;
     float* lse;                          // [heads][rows] or NULL
@@ -59,7 +62,14 @@ __global__ void __launch_bounds__(ForwardShape<kD>::kThreads, ForwardShape<kD>::
 packed_attention_kernel(const __grid_constant__ ForwardParams p)
 {
     using F = ForwardShape<kD>;
-    constexpr int kTiles = F::kTiles, kTileBytes = F::kTileBytes;
+    constexpr int kTiles = F::kTiles, kKeys = F::kKeys, kStages = F::kStages;
+    constexpr int kTmaWarp = 4 * kTiles, kMmaWarp = kTmaWarp + 1;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (warp == kTmaWarp && lane == 0) {
+        prefetch_map(&p.map_q);
+        prefetch_map(&p.map_k);
+        prefetch_map(&p.map_v);
+    }
     pdl_wait_for_predecessors();
     pdl_release_successors();
     const int head = blockIdx.x % p.heads;
@@ -68,19 +78,18 @@ packed_attention_kernel(const __grid_constant__ ForwardParams p)
 
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    auto q_smem = [&](int q) { return smem_base + (uint32_t)(q * kTileBytes); };
-    auto k_smem = [&](int s) { return smem_base + (uint32_t)((kTiles + s) * kTileBytes); };
-    auto v_smem = [&](int s) { return smem_base + (uint32_t)((kTiles + kStages + s) * kTileBytes); };
-    const uint32_t bars = smem_base + (uint32_t)((kTiles + 2 * kStages) * kTileBytes);
-    enum { kQFull = 0, kKFull = 1, kKEmpty = 3, kVFull = 5, kVEmpty = 7, kSFull = 9, kSEmpty = 11, kPFull = 13, kODone = 15, kBars = 17 };
+    auto q_smem = [&](int q) { return smem_base + (uint32_t)(q * F::kQBytes); };
+    auto k_smem = [&](int s) { return smem_base + (uint32_t)(kTiles * F::kQBytes + s * F::kKvBytes); };
+    auto v_smem = [&](int s) { return k_smem(kStages + s); };
+    const uint32_t bars = k_smem(2 * kStages);
+    enum { kQFull = 0, kKvFull = 1, kKvEmpty = kKvFull + kStages, kSFull = kKvEmpty + kStages, kPFull = kSFull + kTiles, kODone = kPFull + kTiles,
+           kBars = kODone + kTiles };
     auto bar = [&](int which, int i) { return bars + (uint32_t)(8 * (which + i)); };
     const uint32_t tmem_holder_addr = bars + 8 * kBars;
     uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(smem_raw + (tmem_holder_addr - smem_u32(smem_raw)));
     volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem_raw + (tmem_holder_addr + 8 - smem_u32(smem_raw)));
-    static_assert(kStages == 2 && 8 * kBars + 16 <= 256, "barriers");
+    static_assert(8 * kBars + 16 <= 256, "barriers");
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr int kTmaWarp = 4 * kTiles, kMmaWarp = kTmaWarp + 1;
     // key tiles of query tile q: none where it has no rows
     auto key_tiles = [&](int q) {
         const int first = tile.first + 128 * q;
@@ -90,117 +99,119 @@ packed_attention_kernel(const __grid_constant__ ForwardParams p)
     };
     const int n0 = key_tiles(0), n1 = kTiles > 1 ? key_tiles(1) : 0;
     const int n = n0 > n1 ? n0 : n1;
-    if (warp == kMmaWarp) {
-        if (lane == 0) {
-            mbar_init(bar(kQFull, 0), 1);
-            for (int s = 0; s < kStages; ++s) {
-                mbar_init(bar(kKFull, s), 1);
-                mbar_init(bar(kKEmpty, s), 1);
-                mbar_init(bar(kVFull, s), 1);
-                mbar_init(bar(kVEmpty, s), 1);
-            }
-            for (int q = 0; q < 2; ++q) {
-                mbar_init(bar(kSFull, q), 1);
-                mbar_init(bar(kSEmpty, q), 4);
-                mbar_init(bar(kPFull, q), 4);
-                mbar_init(bar(kODone, q), 1);
-            }
-            *abort_flag = 0;
-            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        }
-        __syncwarp();
-        tmem_alloc(tmem_holder_addr, F::kTmemCols);
-    }
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    const uint32_t tmem_base = *tmem_holder;
-
+    const int kv_col = head / p.group * kD;
     bool ok = true;
     auto wait = [&](uint32_t b, int count, uint32_t site) {          // for the count-th completion of a barrier, from 0
         ok = mbar_wait(b, (uint32_t)(count & 1), abort_flag, p.dev_status, site);
         ok = __all_sync(0xFFFFFFFFu, ok);
         return ok;
     };
+    // Stage j % kStages has V of tile j and K of tile j + 1, which the products of one step ask for; K of tile 0 comes with Q, into the
+    // stage before the first.
+    auto load_stage = [&](int j) {
+        const int s = j % kStages;
+        mbar_arrive_expect_tx(bar(kKvFull, s), (uint32_t)((j + 1 < n ? 2 : 1) * F::kKvBytes));
+        load_tile<kD, kKeys>(v_smem(s), &p.map_v, bar(kKvFull, s), kv_col, tile.begin + kKeys * j);
+        if (j + 1 < n) load_tile<kD, kKeys>(k_smem(s), &p.map_k, bar(kKvFull, s), kv_col, tile.begin + kKeys * (j + 1));
+    };
     if (warp == kTmaWarp) {
-        // ------------------------------------------------ TMA producer
-        const bool elected = elect_one();
-        const int kv_col = head / p.group * kD;
-        if (elected) {
-            mbar_arrive_expect_tx(bar(kQFull, 0), (uint32_t)((n1 > 0 ? 2 : 1) * kTileBytes));
-            for (int q = 0; q < (n1 > 0 ? 2 : 1); ++q) load_tile<kD, 128>(q_smem(q), &p.map_q, bar(kQFull, 0), head * kD, tile.begin + tile.first + 128 * q);
+        if (lane == 0) {
+            mbar_init(bar(kQFull, 0), 1);
+            for (int s = 0; s < kStages; ++s) {
+                mbar_init(bar(kKvFull, s), 1);
+                mbar_init(bar(kKvEmpty, s), 1);
+            }
+            for (int q = 0; q < kTiles; ++q) {
+                mbar_init(bar(kSFull, q), 1);
+                mbar_init(bar(kPFull, q), 4);
+                mbar_init(bar(kODone, q), 1);
+            }
+            *abort_flag = 0;
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            // the first tiles are on their way before the others of the CTA are ready
+            mbar_arrive_expect_tx(bar(kQFull, 0), (uint32_t)((n1 > 0 ? 2 : 1) * F::kQBytes + F::kKvBytes));
+            load_tile<kD, 128>(q_smem(0), &p.map_q, bar(kQFull, 0), head * kD, tile.begin + tile.first);
+            load_tile<kD, kKeys>(k_smem(kStages - 1), &p.map_k, bar(kQFull, 0), kv_col, tile.begin);
+            if (n1 > 0) load_tile<kD, 128>(q_smem(kTiles - 1), &p.map_q, bar(kQFull, 0), head * kD, tile.begin + tile.first + 128);
+            for (int j = 0; j < kStages - 1 && j < n; ++j) load_stage(j);
         }
         __syncwarp();
-        for (int j = 0; j < n; ++j) {
-            const int s = j % kStages;
-            if (j >= kStages && !wait(bar(kKEmpty, s), j / kStages - 1, 70)) break;
-            if (elected) {
-                mbar_arrive_expect_tx(bar(kKFull, s), (uint32_t)kTileBytes);
-                load_tile<kD, 128>(k_smem(s), &p.map_k, bar(kKFull, s), kv_col, tile.begin + kKeys * j);
-            }
-            __syncwarp();
-            if (j >= kStages && !wait(bar(kVEmpty, s), j / kStages - 1, 71)) break;
-            if (elected) {
-                mbar_arrive_expect_tx(bar(kVFull, s), (uint32_t)kTileBytes);
-                load_tile<kD, 128>(v_smem(s), &p.map_v, bar(kVFull, s), kv_col, tile.begin + kKeys * j);
-            }
+    }
+    if (warp == kMmaWarp) tmem_alloc(tmem_holder_addr, F::kTmemCols);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_holder;
+
+    if (warp == kTmaWarp) {
+        // ------------------------------------------------ TMA producer
+        for (int j = kStages - 1; j < n; ++j) {
+            if (!wait(bar(kKvEmpty, j % kStages), (j + 1) / kStages - 1, 70)) break;
+            if (lane == 0) load_stage(j);
             __syncwarp();
         }
     } else if (warp == kMmaWarp) {
-        // ------------------------------------------------ MMA issuer
+        // ------------------------------------------------ MMA issuer: the first tile's scores, then P V of a tile and the scores of the next, which take its
+        // place.  The tensor core idles while this warp does anything but issue (a wait that is over already costs 60 cycles, a product of 128
+        // columns takes 64), so a step has one wait for K and V, and its products are unrolled with constant addresses and predicates.
+        using Desc = TileDesc<kD>;
         const uint32_t elected = elect_one() ? 1u : 0u;
-        const uint32_t tmem_u = __reduce_or_sync(0xFFFFFFFFu, tmem_base);
-        const int n_of[2] = {n0, n1};
-        // S of key tile j for query tile q; the stage's keys are done with after the last query tile that asks for them
-        auto scores = [&](int q, int j) {
-            if (!wait(bar(kKFull, j % kStages), j / kStages, 72)) return false;
-            tc_fence_after();
+        const uint32_t tmem_u = uniform(tmem_base);
+        const int len = uniform(tile.len), tiles0 = uniform(n0), tiles1 = uniform(n1), tiles = tiles0 > tiles1 ? tiles0 : tiles1;
+        const uint32_t q_desc = Desc::k_major(uniform(smem_base)), k_desc = q_desc + (uint32_t)((kTiles * F::kQBytes) >> 4);
+        const uint32_t v_desc = Desc::template mn_major<kKeys>(uniform(v_smem(0)));
+        auto scores = [&](int q, int s) {
 #pragma unroll
             for (int k = 0; k < kD / 16; ++k)
-                umma_f16_if(tmem_u + (uint32_t)(256 * q), desc_k_major<kD, 128>(q_smem(q), k), desc_k_major<kD, 128>(k_smem(j % kStages), k), p.idesc_s,
-                            (uint32_t)(k != 0), elected);
+                umma_f16_if(tmem_u + (uint32_t)(F::kTileCols * q), Desc::of(q_desc + (uint32_t)(q * (F::kQBytes >> 4)) + Desc::k_step(128, k)),
+                            Desc::of(k_desc + (uint32_t)(s * (F::kKvBytes >> 4)) + Desc::k_step(kKeys, k)), p.idesc_s, (uint32_t)(k != 0), elected);
             umma_commit_if(bar(kSFull, q), elected);
-            if (q == (j < n1 ? 1 : 0)) umma_commit_if(bar(kKEmpty, j % kStages), elected);
-            return true;
         };
-        int zeroed = -1;
-        auto values = [&](int q, int j) {
-            const int s = j % kStages;
-            if (!wait(bar(kVFull, s), j / kStages, 73)) return false;
-            const int left = tile.len - kKeys * j, steps = left >= kKeys ? kKeys / 16 : (left + 15) / 16;
-            if (left < 16 * steps && zeroed != j) {
-                zero_rows<kD, 128>(v_smem(s), left, 16 * steps, lane);
-                fence_proxy_async_smem();
-                __syncwarp();
-                zeroed = j;
+        auto values = [&](int q, int s, bool first, int steps) {
+            const uint32_t t_q = tmem_u + (uint32_t)(F::kTileCols * q);
+            auto step = [&](int k) {
+                umma_f16_ts_if(t_q + F::kOCol, t_q + (uint32_t)(8 * k), Desc::of(v_desc + (uint32_t)(s * (F::kKvBytes >> 4)) + (uint32_t)k * Desc::kRowsStep), p.idesc_o,
+                               k != 0 ? 1u : first ? 0u : 1u, elected);
+            };
+            if (steps >= kKeys / 16) {
+#pragma unroll
+                for (int k = 0; k < kKeys / 16; ++k) step(k);
+            } else {
+#pragma unroll 1
+                for (int k = 0; k < steps; ++k) step(k);
             }
-            if (!wait(bar(kPFull, q), j, 74)) return false;
-            tc_fence_after();
-            for (int k = 0; k < steps; ++k)
-                umma_f16_ts_if(tmem_u + (uint32_t)(256 * q + F::kOCol), tmem_u + (uint32_t)(256 * q + F::kPCol + 8 * k), desc_mn_major<kD, 128>(v_smem(s), k),
-                               p.idesc_o, (uint32_t)(j != 0 || k != 0), elected);
-            umma_commit_if(bar(kODone, q), elected);
-            if (q == (j < n1 ? 1 : 0)) umma_commit_if(bar(kVEmpty, s), elected);
-            return true;
         };
-        wait(bar(kQFull, 0), 0, 75);
-        if constexpr (F::kPOverS) {
-            for (int q = 0; ok && q < kTiles; ++q)
-                if (n_of[q] > 0 && !scores(q, 0)) break;
-            for (int j = 0; ok && j < n; ++j)
+        if (wait(bar(kQFull, 0), 0, 75)) {
+            tc_fence_after();
+            scores(0, kStages - 1);
+            if (kTiles > 1 && tiles1 > 0) scores(1, kStages - 1);
+            umma_commit_if(bar(kKvEmpty, kStages - 1), elected);
+        }
+        int left = len;                                              // keys of the sequence from this tile's first on
+        for (int j0 = 0, round = 0; ok && j0 < tiles; j0 += kStages, ++round) {
+#pragma unroll
+            for (int s = 0; s < kStages; ++s) {
+                const int j = j0 + s;
+                if (!ok || j >= tiles) break;
+                if (!wait(bar(kKvFull, s), round, 73)) break;
+                if (left < kKeys && (left & 15) != 0) {
+                    zero_rows<kD, kKeys>(v_smem(s), left, (left + 15) & ~15, lane);
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                }
 #pragma unroll
                 for (int q = 0; q < kTiles; ++q) {
-                    if (!ok || j >= n_of[q]) continue;
+                    const int tiles_q = q == 0 ? tiles0 : tiles1;
+                    if (j >= tiles_q) continue;
+                    if (!wait(bar(kPFull, q), s, 74)) break;
+                    tc_fence_after();
+                    values(q, s, j == 0, (left + 15) >> 4);
                     // the next scores go over this tile's P: the tensor core takes products in the order they are issued
-                    if (values(q, j) && j + 1 < n_of[q]) scores(q, j + 1);
+                    if (j + 1 < tiles_q) scores(q, s);
+                    else umma_commit_if(bar(kODone, q), elected);
                 }
-        } else {
-            for (int j = 0; ok && j <= n; ++j) {
-                if (j < n) {
-                    if (j > 0 && !wait(bar(kSEmpty, 0), j - 1, 76)) break;
-                    if (!scores(0, j)) break;
-                }
-                if (j > 0 && !values(0, j - 1)) break;
+                umma_commit_if(bar(kKvEmpty, s), elected);
+                left -= kKeys;
             }
         }
         __syncwarp();
@@ -209,154 +220,119 @@ packed_attention_kernel(const __grid_constant__ ForwardParams p)
         const int q = warp >> 2, quarter = warp & 3;
         const int nq = q == 0 ? n0 : n1;
         const int row0 = tile.first + 128 * q + 32 * quarter, row = row0 + lane;       // in the sequence
-        const uint32_t t_lane = tmem_base + (uint32_t)(256 * q) + ((uint32_t)(quarter * 32) << 16);
-        const uint32_t t_p = t_lane + F::kPCol, t_o = t_lane + F::kOCol;
+        const uint32_t t_lane = tmem_base + (uint32_t)(F::kTileCols * q) + ((uint32_t)(quarter * 32) << 16);
+        const uint32_t t_o = t_lane + F::kOCol;
         const int limit = row >= tile.len ? 0 : p.causal ? row + 1 : tile.len;          // keys that take part
         constexpr float kFar = 32768.f;  // no probability above it: inside the 16-bit types and far inside fp32
         const float scale = p.scale_log2;
+        const uint32_t hidden = scale < 0.f ? 0x7f800000u : 0xff800000u;                // times the scale: -inf
         float ref = 0.f;
         uint64_t sum2 = f32x2(0.f, 0.f);
         for (int j = 0; j < nq; ++j) {
+            // with a tile's scores P V of the tile before has ended too: it was issued first
             if (!wait(bar(kSFull, q), j, 77)) break;
             tc_fence_after();
-            const int lim = limit - kKeys * j;                                          // of this tile's keys
-            if (row0 >= tile.len) {
-                // none of the warp's rows exists: it only keeps its place in the barriers, and no tile ahead of the others in any of them
-                if (!F::kPOverS && lane == 0) mbar_arrive(bar(kSEmpty, q));
-                if (j > 0 && !wait(bar(kODone, q), j - 1, 78)) break;
-                if (lane == 0) mbar_arrive(bar(kPFull, q));
-                continue;
-            }
-            const bool whole = __all_sync(0xFFFFFFFFu, lim >= kKeys);
-            const int left = tile.len - kKeys * j;
-            const int read = left >= kKeys ? kKeys : (left + 15) / 16 * 16;             // keys that the second product reads
-            const int most = (int)__reduce_max_sync(0xFFFFFFFFu, (unsigned)(lim < 0 ? 0 : lim > kKeys ? kKeys : lim));
-            const int units = (most + 31) / 32;                                         // of 32 keys with anything to exponentiate
-            auto exp16 = [&](auto masked, const uint32_t* r, int col0, uint64_t& part2, uint32_t (&w)[8]) {
-                const uint64_t scale2 = f32x2(scale, scale), minus_ref = f32x2(-ref, -ref);
+            if (row0 < tile.len) {
+                const int lim = limit - kKeys * j;                                      // of this tile's keys
+                const bool whole = __all_sync(0xFFFFFFFFu, lim >= kKeys);
+                // P lies over the S of chunks that have been read
+                auto chunk = [&](auto masked, int c0) {
+                    uint32_t r[F::kChunk];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float2 a = f32x2_split(f32x2_fma(f32x2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), scale2, minus_ref));
-                    float e0 = exp2_approx(a.x), e1 = exp2_approx(a.y);
-                    if constexpr (decltype(masked)::value) {
-                        if (col0 + 2 * i >= lim) e0 = 0.f;
-                        if (col0 + 2 * i + 1 >= lim) e1 = 0.f;
-                    }
-                    part2 = f32x2_add(part2, f32x2(e0, e1));
-                    w[i] = pack2<kBf16>(e0, e1);
-                }
-            };
-            auto top_of = [&](auto masked, const uint32_t* r, int col0) {
-                float t0 = -INFINITY, t1 = -INFINITY;
-#pragma unroll
-                for (int i = 0; i < 32; i += 2) {
-                    if (!decltype(masked)::value || col0 + i < lim) t0 = fmaxf(t0, __uint_as_float(r[i]) * scale);
-                    if (!decltype(masked)::value || col0 + i + 1 < lim) t1 = fmaxf(t1, __uint_as_float(r[i + 1]) * scale);
-                }
-                return fmaxf(floorf(fmaxf(t0, t1)), -3.0e38f);       // finite for scores of minus infinity
-            };
-            auto rise = [&](float to, int written) {
-                const float up = fminf(to - ref, 127.f);
-                const float factor = __uint_as_float((uint32_t)(127 - (int)up) << 23);          // 2^-up, 0 from 127 on
-                ref = to;
-                sum2 = f32x2_mul(sum2, f32x2(factor, factor));
-                tmem_wait_st();
-                for (int c = 0; c < written; c += 8) {
-                    uint32_t w[8];
-                    tmem_ld_32x32b_x8(t_p + (uint32_t)c, w);
+                    for (int c = 0; c < F::kChunk; c += 32) tmem_ld_32x32b_x32(t_lane + (uint32_t)(c0 + c), r + c);
                     tmem_wait_ld();
+                    if constexpr (decltype(masked)::value) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float2 v = raw2_to_float2<kBf16>(w[i]);
-                        w[i] = pack2<kBf16>(v.x * factor, v.y * factor);
+                        for (int c = 0; c < F::kChunk; ++c)
+                            if (c0 + c >= lim) r[c] = hidden;
                     }
-                    tmem_st_32x32b_x8(t_p + (uint32_t)c, w);
-                }
-                if (j > 0) {
-                    for (int c = 0; c < kD; c += 16) {
-                        uint32_t w[16];
-                        tmem_ld_32x32b_x16(t_o + (uint32_t)c, w);
-                        tmem_wait_ld();
+                    auto top = [&]() {
+                        float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(__uint_as_float(w[i]) * factor);
-                        tmem_st_32x32b_x16(t_o + (uint32_t)c, w);
+                        for (int c = 0; c < F::kChunk; ++c) t[c & 3] = fmaxf(t[c & 3], __uint_as_float(r[c]) * scale);
+                        return fmaxf(floorf(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]))), -3.0e38f);     // finite for scores of minus infinity
+                    };
+                    if (j == 0 && c0 == 0) ref = top();
+                    uint32_t w[F::kChunk / 2];
+                    uint64_t part2;
+                    auto exponentials = [&]() {
+                        const uint64_t scale2 = f32x2(scale, scale), minus_ref = f32x2(-ref, -ref);
+                        uint64_t part[2] = {f32x2(0.f, 0.f), f32x2(0.f, 0.f)};
+#pragma unroll
+                        for (int i = 0; i < F::kChunk / 2; ++i) {
+                            const float2 x = f32x2_split(f32x2_fma(f32x2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), scale2, minus_ref));
+                            const float2 e = make_float2(exp2_approx(x.x), exp2_approx(x.y));
+                            part[i & 1] = f32x2_add(part[i & 1], f32x2(e.x, e.y));
+                            w[i] = pack2<kBf16>(e.x, e.y);
+                        }
+                        part2 = f32x2_add(part[0], part[1]);
+                    };
+                    exponentials();
+                    const float2 part = f32x2_split(part2);
+                    const bool far = part.x + part.y > kFar;
+                    if (__any_sync(0xFFFFFFFFu, far)) {
+                        const float to = far ? fmaxf(top(), ref) : ref;
+                        const float factor = __uint_as_float((uint32_t)(127 - (int)fminf(to - ref, 127.f)) << 23);   // 2^(ref - to), 0 from 2^-127 on
+                        ref = to;
+                        sum2 = f32x2_mul(sum2, f32x2(factor, factor));
+                        tmem_wait_st();
+#pragma unroll 1
+                        for (int c = 0; c < c0 / 2; c += 8) {                           // the tile's P so far
+                            uint32_t o[8];
+                            tmem_ld_32x32b_x8(t_lane + (uint32_t)c, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const float2 v = raw2_to_float2<kBf16>(o[i]);
+                                o[i] = pack2<kBf16>(v.x * factor, v.y * factor);
+                            }
+                            tmem_st_32x32b_x8(t_lane + (uint32_t)c, o);
+                        }
+#pragma unroll 1
+                        for (int c = 0; j > 0 && c < kD; c += 8) {
+                            uint32_t o[8];
+                            tmem_ld_32x32b_x8(t_o + (uint32_t)c, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * factor);
+                            tmem_st_32x32b_x8(t_o + (uint32_t)c, o);
+                        }
+                        exponentials();
                     }
-                }
-            };
-            auto columns = [&](auto masked, const uint32_t* r, int u) {
-                uint64_t part2;
-                auto once = [&]() {
-                    part2 = f32x2(0.f, 0.f);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        uint32_t w[8];
-                        exp16(masked, r + 16 * h, 32 * u + 16 * h, part2, w);
-                        tmem_st_32x32b_x8(t_p + (uint32_t)(16 * u + 8 * h), w);
+                    sum2 = f32x2_add(sum2, part2);
+                    if constexpr (F::kChunk == 64) {
+                        tmem_st_32x32b_x32(t_lane + (uint32_t)(c0 / 2), w);
+                    } else {
+                        tmem_st_32x32b_x16(t_lane + (uint32_t)(c0 / 2), reinterpret_cast<const uint32_t(&)[16]>(w));
                     }
                 };
-                once();
-                const float2 part = f32x2_split(part2);
-                const bool far = part.x + part.y > kFar;
-                if (__any_sync(0xFFFFFFFFu, far)) {
-                    const float top = top_of(masked, r, 32 * u);
-                    rise(far && top > ref ? top : ref, 16 * u);
-                    once();
+                if (whole) {
+#pragma unroll
+                    for (int c0 = 0; c0 < kKeys; c0 += F::kChunk) chunk(std::false_type{}, c0);
+                } else {
+#pragma unroll 1
+                    for (int c0 = 0; c0 < kKeys; c0 += F::kChunk) chunk(std::true_type{}, c0);
                 }
-                sum2 = f32x2_add(sum2, part2);
-            };
-            auto unit = [&](const uint32_t* r, int u) {
-                if (whole) columns(std::false_type{}, r, u);
-                else columns(std::true_type{}, r, u);
-            };
-            uint32_t ra[32], rb[32];
-            tmem_ld_32x32b_x32(t_lane, ra);
-            tmem_wait_ld();
-            if (j == 0) ref = whole ? top_of(std::false_type{}, ra, 0) : top_of(std::true_type{}, ra, 0);
-            // O takes the last tile's product before P is written again
-            if (j > 0 && !wait(bar(kODone, q), j - 1, 78)) break;
-            tc_fence_after();
-            auto scores_read = [&]() {                               // the next tile's scores may take their place
-                if constexpr (!F::kPOverS) {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(kSEmpty, q));
-                }
-            };
-            if (units == 0) scores_read();
-            for (int u = 0; u < units; u += 2) {
-                tmem_wait_ld();
-                if (u + 1 < units) tmem_ld_32x32b_x32(t_lane + (uint32_t)(32 * (u + 1)), rb);
-                else scores_read();
-                unit(ra, u);
-                if (u + 1 < units) {
-                    tmem_wait_ld();
-                    if (u + 2 < units) tmem_ld_32x32b_x32(t_lane + (uint32_t)(32 * (u + 2)), ra);
-                    else scores_read();
-                    unit(rb, u + 1);
-                }
+                tmem_wait_st();
             }
-            for (int c = 32 * units; c < read; c += 16) {
-                const uint32_t w[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
-                tmem_st_32x32b_x8(t_p + (uint32_t)(c / 2), w);
-            }
-            tmem_wait_st();
+            // a warp without rows only keeps its place in the barriers
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(kPFull, q));
         }
-        if (ok && row0 < tile.len && wait(bar(kODone, q), nq - 1, 78)) {
+        if (ok && nq > 0 && row0 < tile.len && wait(bar(kODone, q), 0, 76)) {
             tc_fence_after();
             const float2 both = f32x2_split(sum2);
             const float sum = both.x + both.y, inv = 1.0f / sum;
             if (p.lse != nullptr && row < tile.len)
                 p.lse[(size_t)head * (size_t)p.rows + (size_t)(tile.begin + row)] = (ref + log2f(sum)) * 0.6931471805599453f;
             // Q has been read for the last time: its quarter is the warp's staging room
-            const uint32_t stage = q_smem(q) + (uint32_t)(quarter * (kTileBytes / 4));
+            const uint32_t stage = q_smem(q) + (uint32_t)(quarter * (F::kQBytes / 4));
             uint16_t* dst = p.a + (long long)(tile.begin + row0) * p.a_pitch + head * kD;
+            constexpr int kCols = TileShape<kD>::kCols;
 #pragma unroll
-            for (int c = 0; c < TileShape<kD>::kHalves; ++c)
-                store_rows<kBf16, TileShape<kD>::kCols>(t_o + (uint32_t)(c * TileShape<kD>::kCols), inv, stage, dst + c * TileShape<kD>::kCols, p.a_pitch,
-                                                        tile.len - row0, lane);
+            for (int c = 0; c < kD; c += kCols)
+                store_rows<kBf16, kCols>(t_o + (uint32_t)c, inv, stage, dst + c, p.a_pitch, tile.len - row0, lane);
         }
     }
     if (!ok) let_copies_land();
@@ -493,15 +469,16 @@ elsa_status launch_packed_attention(const elsa_packed_qkv& in, elsa_dtype dtype,
     elsa_status st = device_info(&dev);
     if (st != ELSA_OK) return st;
     ForwardParams p;
-    const int d = in.head_dim;
+    const int d = in.head_dim, keys = d > 64 ? ForwardShape<128>::kKeys : ForwardShape<64>::kKeys;
     if ((st = make_map_heads(&p.map_q, in.q, in.rows, (long long)in.heads * d, in.q_pitch, d, 128, "q")) != ELSA_OK) return st;
-    if ((st = make_map_heads(&p.map_k, in.k, in.rows, (long long)in.kv_heads * d, in.k_pitch, d, 128, "k")) != ELSA_OK) return st;
-    if ((st = make_map_heads(&p.map_v, in.v, in.rows, (long long)in.kv_heads * d, in.v_pitch, d, 128, "v")) != ELSA_OK) return st;
+    if ((st = make_map_heads(&p.map_k, in.k, in.rows, (long long)in.kv_heads * d, in.k_pitch, d, keys, "k")) != ELSA_OK) return st;
+    if ((st = make_map_heads(&p.map_v, in.v, in.rows, (long long)in.kv_heads * d, in.v_pitch, d, keys, "v")) != ELSA_OK) return st;
     p.plan = plan; p.a = a; p.lse = lse; p.a_pitch = a_pitch;
     p.rows = in.rows; p.sequences = sequences; p.heads = in.heads; p.group = in.heads / in.kv_heads;
     p.causal = in.causal ? 1 : 0;
-    p.scale_log2 = in.scale * 1.4426950408889634f;
-    p.idesc_s = packed_idesc(dtype, kKeys, false);
+    // hidden scores are infinite ones times the scale, which must not be zero; 1e-30 makes as much of the others
+    p.scale_log2 = in.scale == 0.f ? 1e-30f : in.scale * 1.4426950408889634f;
+    p.idesc_s = packed_idesc(dtype, keys, false);
     p.idesc_o = packed_idesc(dtype, d, true);
     p.dev_status = dev_status;
     const bool bf = dtype == ELSA_BF16;

@@ -24,22 +24,30 @@ struct PackedTile {
 
 // Tile `index` of the plan's list of 128- or 256-row tiles; false where there is none, or where the plan is not one of these rows
 // and sequences (dev_status then tells).  last_first: tiles of a sequence in reverse order (the costly ones of a causal mask first).
+// index is below plan_capacity(), so the entry may be asked for beside the header.
 template <int kTileRows>
 __device__ __forceinline__ bool plan_tile(const int* plan, int rows, int sequences, int index, bool last_first, uint32_t* dev_status, PackedTile& t)
 {
-    const int4 head = __ldg(reinterpret_cast<const int4*>(plan));
+    const int4* list = reinterpret_cast<const int4*>(plan + kPlanHeader) + (kTileRows == 128 ? 0 : plan_capacity(rows, sequences, 128));
+    int4 head, e;
+    int count;
+    asm volatile("ld.global.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(head.x), "=r"(head.y), "=r"(head.z), "=r"(head.w) : "l"(plan));
+    asm volatile("ld.global.s32 %0, [%1];" : "=r"(count) : "l"(plan + (kTileRows == 128 ? kPlanWord128 : kPlanWord256)));
+    asm volatile("ld.global.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(e.x), "=r"(e.y), "=r"(e.z), "=r"(e.w) : "l"(list + index));
     if (head.x != kPlanMagic || head.y != rows || head.z != sequences) {
         if (dev_status != nullptr && threadIdx.x == 0 && blockIdx.x == 0) atomicCAS(dev_status, 0u, (uint32_t)ELSA_ERR_SHAPE | (79u << 8));
         return false;
     }
-    const int count = kTileRows == 128 ? head.w : __ldg(plan + kPlanWord256);
     if (index >= count) return false;
-    const int4* list = reinterpret_cast<const int4*>(plan + kPlanHeader) + (kTileRows == 128 ? 0 : plan_capacity(rows, sequences, 128));
-    const int4 e = __ldg(list + index);
     t.begin = e.x;
     t.len = e.y;
     t.first = (last_first ? (e.y - 1) / kTileRows - e.z : e.z) * kTileRows;
     return e.x >= 0 && e.y > 0 && t.first >= 0 && t.first < e.y && e.x <= rows - e.y;
+}
+
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map)
+{
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
 }
 
 // A tile of kD columns: kD = 128 lies as two halves of 64 columns, 128-byte rows; kD = 32 has 64-byte rows.
@@ -60,25 +68,31 @@ __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, 
     for (int h = 0; h < T::kHalves; ++h) tma_load_2d(dst + (uint32_t)(h * T::half_bytes(kRows)), map, bar, col + h * T::kCols, row);
 }
 
-// Operand with the reduction along the head's columns, K step k (16 columns).
-template <int kD, int kRows>
-__device__ __forceinline__ uint64_t desc_k_major(uint32_t tile, int k)
-{
+// Matrix descriptors of a tile, as the low word (its address) and a high word that is a constant: the issuing warp adds to the low
+// word alone, from values that it knows to be the same in all lanes (see uniform()), or each product waits for four register moves.
+// K-major: the reduction runs along the head's columns, K step k takes 16 of them.  MN-major: it runs along the tile's rows.
+template <int kD>
+struct TileDesc {
     using T = TileShape<kD>;
-    const uint32_t at = tile + (uint32_t)((k / (T::kCols / 16)) * T::half_bytes(kRows));
-    const uint64_t d = kD >= 64 ? smem_desc_k_major_sw128(at) : smem_desc_k_major_sw64(at);
-    return d + (uint64_t)(2 * (k % (T::kCols / 16)));
-}
+    // stride between groups of eight rows, descriptor version, swizzle of 128 or 64 bytes
+    static constexpr uint32_t kHigh = (uint32_t)((8 * T::kRowBytes) >> 4) | 1u << 14 | (kD >= 64 ? 2u : 4u) << 29;
+    __host__ __device__ static constexpr uint32_t k_step(int rows, int k)
+    {
+        return (uint32_t)(((k / (T::kCols / 16)) * T::half_bytes(rows)) >> 4) + (uint32_t)(2 * (k % (T::kCols / 16)));
+    }
+    static constexpr uint32_t kRowsStep = (16 * T::kRowBytes) >> 4;
+    __device__ static __forceinline__ uint32_t k_major(uint32_t tile) { return (tile >> 4) | 1u << 16; }
+    template <int kRows>
+    __device__ static __forceinline__ uint32_t mn_major(uint32_t tile)
+    {
+        return (tile >> 4) | (uint32_t)(T::half_bytes(kRows) >> 4) << 16;          // leading offset: the next 64 columns
+    }
+    __device__ static __forceinline__ uint64_t of(uint32_t low) { return (uint64_t)kHigh << 32 | low; }
+};
 
-// Operand with the reduction along the tile's rows, K step k (16 rows).
-template <int kD, int kRows>
-__device__ __forceinline__ uint64_t desc_mn_major(uint32_t tile, int k)
-{
-    using T = TileShape<kD>;
-    const uint64_t d = kD >= 64 ? smem_desc_mn_major_sw128(tile, (uint32_t)T::half_bytes(kRows))
-                                : smem_desc_mn_major_sw64(tile, (uint32_t)T::half_bytes(kRows));
-    return d + (uint64_t)(k * ((16 * T::kRowBytes) >> 4));
-}
+// A value that all lanes of the (converged) warp hold, in a form that the compiler knows to be one.
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __reduce_or_sync(0xFFFFFFFFu, v); }
+__device__ __forceinline__ int uniform(int v) { return (int)__reduce_or_sync(0xFFFFFFFFu, (unsigned)v); }
 
 // Rows [from, to) of a tile set to zero by a warp: what lies behind a sequence's end may be anything, and zero times NaN is NaN.
 template <int kD, int kRows>
@@ -91,6 +105,18 @@ __device__ __forceinline__ void zero_rows(uint32_t tile, int from, int to, int l
         for (int i = lane; i < (to - from) * kVecs; i += 32)
             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + (uint32_t)(h * T::half_bytes(kRows) + from * T::kRowBytes + i * 16)), "r"(0)
                          : "memory");
+}
+
+__device__ __forceinline__ void tmem_st_32x32b_x32(uint32_t taddr, const uint32_t* r)
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+        "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]),
+        "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
 }
 
 // A warp's 32 lanes x kCols fp32 columns of tensor memory, times a factor per lane, rounded once, to the first rows_left of 32

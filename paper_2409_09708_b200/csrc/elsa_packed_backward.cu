@@ -18,6 +18,7 @@
 // What bounds it: per tile 512 cycles of exponentials, and products of 640 (384) cycles for heads of 64 columns, 1280 (1024) for 128:
 // the shared memory's 128 bytes a cycle bound S and T (6 KB for each 16 columns of the head, 48 cycles against the tensor core's 32).
 #include <atomic>
+#include <type_traits>
 
 #include "elsa_packed.cuh"
 
@@ -32,7 +33,7 @@ struct BackwardShape {
     static constexpr int kThreads = 2 * 128 + 64;
     static constexpr int kKeptBytes = TileShape<kD>::bytes(128), kWalkBytes = TileShape<kD>::bytes(kWalk);
     static constexpr int kAcc1 = 256, kAcc2 = 256 + kD;              // tensor-memory columns; stage g: S at 128 g, T at 128 g + 64
-    static constexpr int kVectorBytes = 2 * kWalk * 4;               // -lse log2(e), delta
+    static constexpr int kVectorBytes = 2 * kWalk * 4;               // -lse log2(e), -delta
     static constexpr int kSmemBytes = 2 * kKeptBytes + kRing * (2 * kWalkBytes + kVectorBytes) + 1024 /* delta of the kept rows */ +
                                       1024 /* alignment */ + 256 /* barriers */;
 };
@@ -45,7 +46,7 @@ struct BackwardParams {
     const uint16_t* da;
     const float* lse;                    // [heads][rows]
     float* minus_lse;                    // [heads][rows]: -lse log2(e), made by the dq kernel for the other
-    float* delta;                        // [heads][rows]
+    float* minus_delta;                  // [heads][rows]
     uint16_t* out1;                      // dv
     uint16_t* out2;                      // dq or dk
     long long a_pitch, da_pitch, out1_pitch, out2_pitch;
@@ -159,21 +160,26 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
                     const bool in = row + c < tile.len;
                     const uint32_t dst = vectors + (uint32_t)(s * B::kVectorBytes + 4 * c);
                     copy_word(dst, p.minus_lse + (in ? at + c : 0), in);
-                    copy_word(dst + 4 * kWalk, p.delta + (in ? at + c : 0), in);
+                    copy_word(dst + 4 * kWalk, p.minus_delta + (in ? at + c : 0), in);
                 }
                 copies_arrive(bar(kYFull, s));
             }
         }
     } else if (warp == kMmaWarp) {
         // ------------------------------------------------ MMA issuer: S and T of tile it, then the sums of tile it - 1
+        using Desc = TileDesc<kD>;
         const uint32_t elected = elect_one() ? 1u : 0u;
-        const uint32_t tmem_u = __reduce_or_sync(0xFFFFFFFFu, tmem_base);
+        const uint32_t tmem_u = uniform(tmem_base);
+        const int tiles = uniform(n), tiles_a_head = uniform(per_head), first_left = uniform(tile.len - walk_from * kWalk);
+        const uint32_t x1_desc = Desc::k_major(uniform(smem_base)), x2_desc = x1_desc + (uint32_t)(B::kKeptBytes >> 4);
+        const uint32_t y1_rows = Desc::k_major(uniform(y1_smem(0))), y1_cols = Desc::template mn_major<kWalk>(uniform(y1_smem(0)));
+        constexpr uint32_t kY2 = (uint32_t)(B::kWalkBytes >> 4);
+        int left = first_left, t = 0, left_before = 0;               // rows of the sequence from this tile's first on; the tile before
         wait(bar(kXFull, 0), 0, 81);
-        for (int it = 0; ok && it <= n; ++it) {
-            if (it < n) {
+        for (int it = 0; ok && it <= tiles; ++it) {
+            if (it < tiles) {
                 const int s = it % kRing, g = it & 1;
                 if (!wait(bar(kYFull, s), it / kRing, 82)) break;
-                const int left = tile.len - (walk_from + it % per_head) * kWalk;
                 if (left < kWalk && (left & 15) != 0) {
                     zero_rows<kD, kWalk>(y1_smem(s), left, (left + 15) & ~15, lane);
                     zero_rows<kD, kWalk>(y2_smem(s), left, (left + 15) & ~15, lane);
@@ -181,31 +187,37 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
                     __syncwarp();
                 }
                 tc_fence_after();
-                const uint32_t t_s = tmem_u + (uint32_t)(128 * g);
+                const uint32_t t_s = tmem_u + (uint32_t)(128 * g), y_at = y1_rows + (uint32_t)(s * 2) * kY2;
 #pragma unroll
                 for (int k = 0; k < kD / 16; ++k)
-                    umma_f16_if(t_s, desc_k_major<kD, 128>(x1_smem, k), desc_k_major<kD, kWalk>(y1_smem(s), k), p.idesc_s, (uint32_t)(k != 0), elected);
+                    umma_f16_if(t_s, Desc::of(x1_desc + Desc::k_step(128, k)), Desc::of(y_at + Desc::k_step(kWalk, k)), p.idesc_s, (uint32_t)(k != 0), elected);
 #pragma unroll
                 for (int k = 0; k < kD / 16; ++k)
-                    umma_f16_if(t_s + 64, desc_k_major<kD, 128>(x2_smem, k), desc_k_major<kD, kWalk>(y2_smem(s), k), p.idesc_s, (uint32_t)(k != 0), elected);
+                    umma_f16_if(t_s + 64, Desc::of(x2_desc + Desc::k_step(128, k)), Desc::of(y_at + kY2 + Desc::k_step(kWalk, k)), p.idesc_s, (uint32_t)(k != 0), elected);
                 umma_commit_if(bar(kSFull, g), elected);
             }
             if (it > 0) {
                 const int m = it - 1, s = m % kRing, g = m & 1;
                 if (!wait(bar(kPFull, g), m >> 1, 83)) break;
                 tc_fence_after();
-                const int left = tile.len - (walk_from + m % per_head) * kWalk;
-                const int steps = left >= kWalk ? kWalk / 16 : (left + 15) / 16;
-                const uint32_t t_s = tmem_u + (uint32_t)(128 * g);
+                const int steps = left_before >= kWalk ? kWalk / 16 : (left_before + 15) / 16;
+                const uint32_t t_s = tmem_u + (uint32_t)(128 * g), y_at = y1_cols + (uint32_t)(s * 2) * kY2;
                 if constexpr (kKeys) {
-                    for (int k = 0; k < steps; ++k)
-                        umma_f16_ts_if(tmem_u + B::kAcc1, t_s + (uint32_t)(8 * k), desc_mn_major<kD, kWalk>(y2_smem(s), k), p.idesc_acc, (uint32_t)(m != 0 || k != 0), elected);
+#pragma unroll
+                    for (int k = 0; k < kWalk / 16; ++k)
+                        umma_f16_ts_if(tmem_u + B::kAcc1, t_s + (uint32_t)(8 * k), Desc::of(y_at + kY2 + k * Desc::kRowsStep), p.idesc_acc,
+                                       (uint32_t)(m != 0 || k != 0), k < steps ? elected : 0u);
                 }
-                for (int k = 0; k < steps; ++k)
-                    umma_f16_ts_if(tmem_u + B::kAcc2, t_s + (uint32_t)(64 + 8 * k), desc_mn_major<kD, kWalk>(y1_smem(s), k), p.idesc_acc, (uint32_t)(m != 0 || k != 0), elected);
+#pragma unroll
+                for (int k = 0; k < kWalk / 16; ++k)
+                    umma_f16_ts_if(tmem_u + B::kAcc2, t_s + (uint32_t)(64 + 8 * k), Desc::of(y_at + k * Desc::kRowsStep), p.idesc_acc,
+                                   (uint32_t)(m != 0 || k != 0), k < steps ? elected : 0u);
                 umma_commit_if(bar(kYEmpty, s), elected);
-                if (m == n - 1) umma_commit_if(bar(kDone, 0), elected);
+                if (m == tiles - 1) umma_commit_if(bar(kDone, 0), elected);
             }
+            left_before = left;
+            left -= kWalk;
+            if (++t == tiles_a_head) { t = 0; left = first_left; }
         }
         __syncwarp();
     } else {
@@ -214,7 +226,7 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
         const int row0 = tile.first + 32 * quarter, row = row0 + lane;                 // kept row, in the sequence
         const bool exists = row < tile.len;
         const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16);
-        float minus_lse = 0.f, delta = 0.f;
+        float minus_lse = 0.f, minus_delta = 0.f;
         if constexpr (!kKeys) {
             // delta: half a row by each group
             const size_t at = (size_t)head * (size_t)p.rows + (size_t)(tile.begin + row);
@@ -240,10 +252,10 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
             float first, second;
             asm volatile("ld.shared.f32 %0, [%1];" : "=f"(first) : "r"(mine) : "memory");
             asm volatile("ld.shared.f32 %0, [%1];" : "=f"(second) : "r"(mine + 512u) : "memory");
-            delta = first + second;
+            minus_delta = -(first + second);
             if (g == 0 && exists) {
                 p.minus_lse[at] = minus_lse;
-                p.delta[at] = delta;
+                p.minus_delta[at] = minus_delta;
             }
         }
         const uint64_t scale2 = f32x2(p.scale_log2, p.scale_log2);
@@ -262,8 +274,7 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
                 const int hi = kKeys ? kWalk : (p.causal && row + 1 < tile.len ? row + 1 : tile.len) - walked;
                 const bool whole = __all_sync(0xFFFFFFFFu, lo <= 0 && hi >= kWalk);
                 const uint32_t vec = vectors + (uint32_t)(s * B::kVectorBytes);
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
+                auto unit = [&](auto masked, int u) {
                     uint32_t rs[32], rt[32];
                     tmem_ld_32x32b_x32(t_lane + (uint32_t)(128 * g + 32 * u), rs);
                     tmem_ld_32x32b_x32(t_lane + (uint32_t)(128 * g + 64 + 32 * u), rt);
@@ -271,21 +282,21 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
                     uint32_t wp[16], wd[16];
 #pragma unroll
                     for (int i = 0; i < 16; i += 2) {
-                        float4 l4 = make_float4(minus_lse, minus_lse, minus_lse, minus_lse), d4 = make_float4(delta, delta, delta, delta);
+                        uint64_t l2[2], d2[2];               // -lse log2(e) and -delta of two columns each
                         if constexpr (kKeys) {
-                            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(l4.x), "=f"(l4.y), "=f"(l4.z), "=f"(l4.w) : "r"(vec + (uint32_t)(128 * u + 8 * i)));
-                            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(d4.x), "=f"(d4.y), "=f"(d4.z), "=f"(d4.w) : "r"(vec + (uint32_t)(4 * kWalk + 128 * u + 8 * i)));
+                            asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(l2[0]), "=l"(l2[1]) : "r"(vec + (uint32_t)(128 * u + 8 * i)));
+                            asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(d2[0]), "=l"(d2[1]) : "r"(vec + (uint32_t)(4 * kWalk + 128 * u + 8 * i)));
+                        } else {
+                            l2[0] = l2[1] = f32x2(minus_lse, minus_lse);
+                            d2[0] = d2[1] = f32x2(minus_delta, minus_delta);
                         }
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            const int c = 2 * (i + h);
-                            const uint64_t l2 = h == 0 ? f32x2(l4.x, l4.y) : f32x2(l4.z, l4.w);
-                            const uint64_t d2 = h == 0 ? f32x2(-d4.x, -d4.y) : f32x2(-d4.z, -d4.w);
-                            const float2 e = f32x2_split(f32x2_fma(f32x2(__uint_as_float(rs[c]), __uint_as_float(rs[c + 1])), scale2, l2));
+                            const int c = 2 * (i + h), col = 32 * u + c;
+                            const float2 e = f32x2_split(f32x2_fma(f32x2(__uint_as_float(rs[c]), __uint_as_float(rs[c + 1])), scale2, l2[h]));
                             float2 pp = make_float2(exp2_approx(e.x), exp2_approx(e.y));
-                            float2 ds = f32x2_split(f32x2_mul(f32x2(pp.x, pp.y), f32x2_add(f32x2(__uint_as_float(rt[c]), __uint_as_float(rt[c + 1])), d2)));
-                            if (!whole) {
-                                const int col = 32 * u + c;
+                            float2 ds = f32x2_split(f32x2_mul(f32x2(pp.x, pp.y), f32x2_add(f32x2(__uint_as_float(rt[c]), __uint_as_float(rt[c + 1])), d2[h])));
+                            if constexpr (decltype(masked)::value) {
                                 if (col < lo || col >= hi) pp.x = ds.x = 0.f;
                                 if (col + 1 < lo || col + 1 >= hi) pp.y = ds.y = 0.f;
                             }
@@ -295,6 +306,13 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
                     }
                     if constexpr (kKeys) tmem_st_32x32b_x16(t_lane + (uint32_t)(128 * g + 16 * u), wp);
                     tmem_st_32x32b_x16(t_lane + (uint32_t)(128 * g + 64 + 16 * u), wd);
+                };
+                if (whole) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) unit(std::false_type{}, u);
+                } else {
+#pragma unroll 1
+                    for (int u = 0; u < 2; ++u) unit(std::true_type{}, u);
                 }
                 tmem_wait_st();
             }
@@ -379,7 +397,7 @@ elsa_status launch_packed_attention_backward(const elsa_packed_qkv& in, elsa_dty
     BackwardParams q, k;
     q.plan = plan; q.a = a; q.da = da; q.lse = lse;
     q.minus_lse = static_cast<float*>(workspace);
-    q.delta = reinterpret_cast<float*>(static_cast<char*>(workspace) + packed_attention_workspace(rows, in.heads) / 2);
+    q.minus_delta = reinterpret_cast<float*>(static_cast<char*>(workspace) + packed_attention_workspace(rows, in.heads) / 2);
     q.a_pitch = a_pitch; q.da_pitch = da_pitch;
     q.rows = rows; q.sequences = sequences; q.heads = in.heads; q.kv_heads = in.kv_heads; q.group = in.heads / in.kv_heads;
     q.causal = in.causal ? 1 : 0;
