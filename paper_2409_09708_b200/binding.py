@@ -128,24 +128,6 @@ class ElsaBlockWeights(ctypes.Structure):
 
 _backward_ws = _sig("elsa_backward_workspace_bytes", _sz, [_i, _i, _i, _i, _i, _i])
 _backward = _sig("elsa_nm_linear_backward", _i, [_vp, _vp, _i, _vp, _vp, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _sz, _vp, _vp])
-_elsa_host.bind({fn.__name__: ctypes.cast(fn, _vp).value
-                 for fn in (_linear, _linear_masked, _linear_i8, _backward, _compress, _compress_levels, _values_bytes, _index_bytes,
-                            _workspace_bytes, _workspace_bytes_i8, _backward_ws)})
-BLOCK_REGIONS = ("x1", "qkv", "a", "x2", "x3", "h", "t", "workspace")
-_bw = ctypes.POINTER(ElsaBlockWeights)
-_block_scratch = _sig("elsa_vit_block_scratch_bytes", _sz, [_i, _i, _i, _bw, _i, ctypes.POINTER(_sz)])
-_block_qkv = _sig("elsa_vit_block_qkv", _i, [_vp, _i, _i, _i, _bw, _i, _vp, _sz, _vp, _vp])
-_block_rest = _sig("elsa_vit_block_rest", _i, [_vp, _i, _i, _i, _bw, _i, _vp, _vp, _sz, _vp, _vp])
-_block = _sig("elsa_vit_block", _i, [_vp, _i, _i, _i, _bw, _i, _vp, _vp, _sz, _vp, _vp])
-_block_attn = _sig("elsa_vit_block_attn", _i, [_vp, _i, _i, _i, _i, _i, _bw, _i, _vp, _vp, _sz, _vp, _vp])
-_attention = _sig("elsa_attention", _i, [_vp, _i, _i, _i, _i, _i, _vp, _vp, _vp])
-_window_attention = _sig("elsa_window_attention", _i, [_vp, _i, _i, _i, _i, _vp, _i, _vp, _i, _i, _vp, _vp, _vp])
-class ElsaSwinAttn(ctypes.Structure):
-    _fields_ = [("H", _i), ("W", _i), ("window", _i), ("shift", _i), ("rel_bias", _vp), ("mask", _vp), ("bias_pitch", _i),
-                ("pack", _i)]
-
-
-_fp = ctypes.POINTER(ctypes.c_float)
 _ll = ctypes.c_longlong
 ROTARY_MAX_AXES, ROTARY_MAX_PAIRS = 4, 128
 
@@ -171,6 +153,25 @@ _packed = _sig("elsa_packed_attention", _i, [ctypes.POINTER(ElsaPackedQkv), _i, 
 _packed_ws = _sig("elsa_packed_attention_workspace_bytes", _sz, [_i, _i])
 _packed_backward = _sig("elsa_packed_attention_backward", _i, [ctypes.POINTER(ElsaPackedQkv), _i, _vp, _i, _vp, _ll, _vp, _vp, _ll, _vp, _ll, _vp,
                                                                _ll, _vp, _ll, _vp, _sz, _vp, _vp])
+_elsa_host.bind({fn.__name__: ctypes.cast(fn, _vp).value
+                 for fn in (_linear, _linear_masked, _linear_i8, _backward, _compress, _compress_levels, _values_bytes, _index_bytes,
+                            _workspace_bytes, _workspace_bytes_i8, _backward_ws, _layer_norm, _layer_norm_backward, _layer_norm_backward_ws, _rotary,
+                            _packed, _packed_backward, _packed_ws)})
+BLOCK_REGIONS = ("x1", "qkv", "a", "x2", "x3", "h", "t", "workspace")
+_bw = ctypes.POINTER(ElsaBlockWeights)
+_block_scratch = _sig("elsa_vit_block_scratch_bytes", _sz, [_i, _i, _i, _bw, _i, ctypes.POINTER(_sz)])
+_block_qkv = _sig("elsa_vit_block_qkv", _i, [_vp, _i, _i, _i, _bw, _i, _vp, _sz, _vp, _vp])
+_block_rest = _sig("elsa_vit_block_rest", _i, [_vp, _i, _i, _i, _bw, _i, _vp, _vp, _sz, _vp, _vp])
+_block = _sig("elsa_vit_block", _i, [_vp, _i, _i, _i, _bw, _i, _vp, _vp, _sz, _vp, _vp])
+_block_attn = _sig("elsa_vit_block_attn", _i, [_vp, _i, _i, _i, _i, _i, _bw, _i, _vp, _vp, _sz, _vp, _vp])
+_attention = _sig("elsa_attention", _i, [_vp, _i, _i, _i, _i, _i, _vp, _vp, _vp])
+_window_attention = _sig("elsa_window_attention", _i, [_vp, _i, _i, _i, _i, _vp, _i, _vp, _i, _i, _vp, _vp, _vp])
+class ElsaSwinAttn(ctypes.Structure):
+    _fields_ = [("H", _i), ("W", _i), ("window", _i), ("shift", _i), ("rel_bias", _vp), ("mask", _vp), ("bias_pitch", _i),
+                ("pack", _i)]
+
+
+_fp = ctypes.POINTER(ctypes.c_float)
 _swin_mask = _sig("elsa_swin_mask", _i, [_i, _i, _i, _i, _i, _i, _fp])
 _swin_pack_bias = _sig("elsa_swin_pack_bias", _i, [_fp, _i, _i, _i, _i, _fp])
 _swin_block = _sig("elsa_swin_block", _i, [_vp, _i, _i, _i, _i, _bw, ctypes.POINTER(ElsaSwinAttn), _i, _vp, _vp, _sz, _vp, _vp])
@@ -484,62 +485,14 @@ def elsa_window_attention(qkv, tokens, heads, bias, mask=None, a=None, dev_statu
 
 # ---- LayerNorm, rotary positions and attention over packed sequences, with their gradients
 
-def _same_place(*tensors):
-    """The library launches on the current device: every tensor of a call has to be there."""
-    here = None
-    for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise ValueError("CUDA tensor expected, got one on %s" % t.device)
-        if here is None:
-            here = torch.cuda.current_device()
-        if t.get_device() != here:
-            raise ValueError("tensor on %s, the current device is cuda:%d" % (t.device, here))
-
-
-def _same_dtype(*tensors):
-    code = dtype_code(tensors[0].dtype)
-    for t in tensors[1:]:
-        if t is not None and t.dtype != tensors[0].dtype:
-            raise TypeError("%s expected, got %s" % (tensors[0].dtype, t.dtype))
-    return code
-
-
-def _shape(t, shape, name):
-    if t is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError("%s: shape %s expected, got %s" % (name, tuple(shape), tuple(t.shape)))
-
-
-def _pitch(t, name):
-    """(address, values between rows) of a matrix whose rows are contiguous, such as the columns of one third of qkv."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError("%s: a matrix with contiguous rows expected" % name)
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), (t.shape[1] + 7) // 8 * 8)
+def _handle(stream):
+    return None if stream is None else stream.cuda_stream           # None: the extension module asks for the current one
 
 
 def elsa_layer_norm(x, gain, bias, eps=1e-6, residual=None, want_stats=False, y=None, s=None, stats=None, stream=None):
     """(y, s, stats) of x [rows, dim]: s = x + residual where there is one (x itself otherwise), y = LayerNorm(s), stats
     [rows, 2] its mean and 1 / sqrt(var + eps) where asked for (None otherwise)."""
-    code = _same_dtype(x, gain, bias, residual, y, s)
-    _same_place(x, gain, bias, residual, y, s, stats)
-    rows, dim = x.shape
-    for t, name in ((gain, "gain"), (bias, "bias")):
-        _shape(t, (dim,), name)
-    for t, name in ((residual, "residual"), (y, "y"), (s, "s")):
-        _shape(t, (rows, dim), name)
-    if residual is None and s is not None:
-        raise ValueError("s is written where there is a residual")
-    if stats is not None and (stats.dtype != torch.float32 or tuple(stats.shape) != (rows, 2)):
-        raise ValueError("stats: fp32 [%d, 2] expected" % rows)
-    if y is None:
-        y = torch.empty_like(x)
-    if residual is not None and s is None:
-        s = torch.empty_like(x)
-    if want_stats and stats is None:
-        stats = torch.empty((rows, 2), dtype=torch.float32, device=x.device)
-    _check(_layer_norm(_ptr(x), _ptr(residual), _ptr(gain), _ptr(bias), rows, dim, eps, code, _ptr(s), _ptr(y), _ptr(stats), _stream(stream)))
-    return y, x if residual is None else s, stats
+    return _result(_elsa_host.layer_norm(x, gain, bias, eps, residual, want_stats, y, s, stats, _handle(stream)))
 
 
 def elsa_layer_norm_backward_workspace_bytes(rows, dim) -> int:
@@ -549,25 +502,8 @@ def elsa_layer_norm_backward_workspace_bytes(rows, dim) -> int:
 def elsa_layer_norm_backward(dy, s, gain, stats, ds=None, want=("dx", "dgain", "dbias"), dx=None, workspace=None, stream=None):
     """(dx, dgain, dbias), None for the ones not in `want`; s and stats as elsa_layer_norm returned them, ds the gradient that
     arrives at s along the residual path (added to dx)."""
-    code = _same_dtype(dy, s, gain, ds, dx)
-    _same_place(dy, s, gain, stats, ds, dx, workspace)
-    rows, dim = dy.shape
-    for t, name in ((s, "s"), (ds, "ds"), (dx, "dx")):
-        _shape(t, (rows, dim), name)
-    _shape(gain, (dim,), "gain")
-    if stats is None or stats.dtype != torch.float32 or tuple(stats.shape) != (rows, 2):
-        raise ValueError("stats: fp32 [%d, 2] expected" % rows)
-    if "dx" not in want:
-        dx = None
-    elif dx is None:
-        dx = torch.empty_like(dy)
-    dgain = torch.empty_like(gain) if "dgain" in want else None
-    dbias = torch.empty_like(gain) if "dbias" in want else None
-    if workspace is None and (dgain is not None or dbias is not None):
-        workspace = alloc_workspace(elsa_layer_norm_backward_workspace_bytes(rows, dim), dy.device)
-    _check(_layer_norm_backward(_ptr(dy), _ptr(s), _ptr(stats), _ptr(gain), _ptr(ds), rows, dim, code, _ptr(dx), _ptr(dgain), _ptr(dbias),
-                                _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)))
-    return dx, dgain, dbias
+    return _result(_elsa_host.layer_norm_backward(dy, s, gain, stats, ds, "dx" in want, "dgain" in want, "dbias" in want, dx, workspace,
+                                                  _handle(stream)))
 
 
 def make_rotary_plan(head_dim, sections, base=10000.0, shared=False, interleaved=False):
@@ -582,34 +518,16 @@ def make_rotary_plan(head_dim, sections, base=10000.0, shared=False, interleaved
 def elsa_rotary(x, positions, plan, y=None, inverse=False, stream=None):
     """y [rows, heads * head_dim] = the heads of x (its columns may be part of a wider tensor) turned by positions [rows, axes];
     y = x turns in place.  inverse: the gradient."""
-    code = _same_dtype(x, y) if y is not None else dtype_code(x.dtype)
-    _same_place(x, positions, y)
-    xp, x_pitch = _pitch(x, "x")
-    rows, width = x.shape
-    if width == 0 or width % plan.head_dim:
-        raise ValueError("x: %d columns are no heads of %d" % (width, plan.head_dim))
-    if positions.dtype != torch.int32:
-        raise TypeError("positions: int32 expected, got %s" % positions.dtype)
-    _shape(positions, (rows, plan.axes), "positions")
-    if y is None:
-        y = torch.empty((rows, width), dtype=x.dtype, device=x.device)
-    _shape(y, (rows, width), "y")
-    yp, y_pitch = _pitch(y, "y")
-    _check(_rotary(xp, x_pitch, _ptr(positions), ctypes.byref(plan), rows, width // plan.head_dim, 1 if inverse else 0, code, yp, y_pitch,
-                   _stream(stream)))
-    return y
+    return _result(_elsa_host.rotary(x, positions, ctypes.addressof(plan), y, inverse, _handle(stream)))
 
 
 class PackedPlan:
-    """Where the sequences of a packed batch lie, cut into tiles once for all calls on that batch (see make_packed_plan)."""
+    """Where the sequences of a packed batch lie, cut into tiles once for all calls on that batch (see make_packed_plan).  full: every
+    row belongs to a sequence; otherwise outputs that a call allocates itself start as zeros, since it leaves the other rows as they are."""
 
     def __init__(self, offsets, rows, full, buffer):
         self.offsets, self.rows, self.full, self.buffer = offsets, rows, full, buffer
         self.sequences = offsets.numel() - 1
-
-    def empty(self, width, dtype):
-        """Uninitialised [rows, width]; zeros where rows may belong to no sequence, which the calls leave as they are."""
-        return (torch.empty if self.full else torch.zeros)((self.rows, width), dtype=dtype, device=self.buffer.device)
 
 
 def make_packed_plan(offsets, rows=None, device="cuda", dev_status=None, stream=None):
@@ -626,24 +544,12 @@ def make_packed_plan(offsets, rows=None, device="cuda", dev_status=None, stream=
         offsets = torch.tensor(host, dtype=torch.int32).to(device)
     elif offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.numel() < 2 or rows is None:
         raise ValueError("offsets on the device: an int32 vector of two or more, and the number of rows")
-    _same_place(offsets, dev_status)
+    if offsets.get_device() != torch.cuda.current_device():
+        raise ValueError("offsets on %s, the current device is cuda:%d" % (offsets.device, torch.cuda.current_device()))
     nbytes = int(_packed_plan_bytes(rows, offsets.numel() - 1))
     buffer = torch.empty((max(nbytes, 16),), dtype=torch.uint8, device=offsets.device)
     _check(_packed_plan(_ptr(offsets), offsets.numel() - 1, rows, _ptr(buffer), nbytes, _ptr(dev_status), _stream(stream)))
     return PackedPlan(offsets, rows, full, buffer)
-
-
-def _packed_args(q, k, v, plan, heads, kv_heads, causal, scale):
-    code = _same_dtype(q, k, v)
-    if heads <= 0 or kv_heads <= 0 or q.dim() != 2 or q.shape[1] % heads:
-        raise ValueError("q: %s is no matrix of %d heads" % (tuple(q.shape), heads))
-    width = q.shape[1] // heads
-    _shape(q, (plan.rows, heads * width), "q")
-    for t, name in ((k, "k"), (v, "v")):
-        _shape(t, (plan.rows, kv_heads * width), name)
-    (qp, ql), (kp, kl), (vp, vl) = _pitch(q, "q"), _pitch(k, "k"), _pitch(v, "v")
-    return code, width, ElsaPackedQkv(qp, kp, vp, ql, kl, vl, plan.rows, heads, kv_heads, width, 1 if causal else 0,
-                                      width ** -0.5 if scale is None else scale)
 
 
 def elsa_packed_attention(q, k, v, plan, heads, kv_heads=None, causal=False, scale=None, a=None, want_lse=False, lse=None, dev_status=None,
@@ -651,45 +557,17 @@ def elsa_packed_attention(q, k, v, plan, heads, kv_heads=None, causal=False, sca
     """(a, lse): a [rows, heads * head_dim], softmax attention within the sequences of `plan`; q [rows, heads * head_dim], k and v
     [rows, kv_heads * head_dim] may be columns of one qkv tensor.  scale: 1 / sqrt(head_dim) unless given.  lse [heads, rows]
     fp32 where asked for, as the gradient needs it (None otherwise)."""
-    kv_heads = heads if kv_heads is None else kv_heads
-    _same_place(q, k, v, a, lse, plan.buffer, dev_status)
-    code, width, args = _packed_args(q, k, v, plan, heads, kv_heads, causal, scale)
-    if a is None:
-        a = plan.empty(heads * width, q.dtype)
-    elif a.dtype != q.dtype:
-        raise TypeError("a: %s expected, got %s" % (q.dtype, a.dtype))
-    _shape(a, (plan.rows, heads * width), "a")
-    if want_lse and lse is None:
-        lse = torch.empty((heads, plan.rows), dtype=torch.float32, device=q.device)
-    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (heads, plan.rows)):
-        raise ValueError("lse: fp32 [%d, %d] expected" % (heads, plan.rows))
-    ap, al = _pitch(a, "a")
-    _check(_packed(ctypes.byref(args), code, _ptr(plan.buffer), plan.sequences, ap, al, _ptr(lse), _ptr(dev_status), _stream(stream)))
-    return a, lse
+    return _result(_elsa_host.packed_attention(q, k, v, plan.buffer, plan.rows, plan.sequences, plan.full, heads, heads if kv_heads is None else kv_heads,
+                                               causal, scale, a, want_lse, lse, dev_status, _handle(stream)))
 
 
 def elsa_packed_attention_backward(da, q, k, v, a, lse, plan, heads, kv_heads=None, causal=False, scale=None, dq=None, dk=None, dv=None,
                                    workspace=None, dev_status=None, stream=None):
     """(dq, dk, dv) for the gradient da arriving at a; a and lse as elsa_packed_attention returned them.  dq, dk and dv may be given,
     as columns of one tensor too."""
-    kv_heads = heads if kv_heads is None else kv_heads
-    _same_place(da, q, k, v, a, lse, dq, dk, dv, workspace, plan.buffer, dev_status)
-    code, width, args = _packed_args(q, k, v, plan, heads, kv_heads, causal, scale)
-    _same_dtype(q, da, a, dq, dk, dv)
-    dq = plan.empty(heads * width, q.dtype) if dq is None else dq
-    dk = plan.empty(kv_heads * width, q.dtype) if dk is None else dk
-    dv = plan.empty(kv_heads * width, q.dtype) if dv is None else dv
-    for t, n, name in ((da, heads, "da"), (a, heads, "a"), (dq, heads, "dq"), (dk, kv_heads, "dk"), (dv, kv_heads, "dv")):
-        _shape(t, (plan.rows, n * width), name)
-    if lse is None or lse.dtype != torch.float32 or tuple(lse.shape) != (heads, plan.rows):
-        raise ValueError("lse: fp32 [%d, %d] expected" % (heads, plan.rows))
-    if workspace is None:
-        workspace = alloc_workspace(int(_packed_ws(plan.rows, heads)), q.device)
-    (ap, al), (gp, gl) = _pitch(a, "a"), _pitch(da, "da")
-    (qp, ql), (kp, kl), (vp, vl) = _pitch(dq, "dq"), _pitch(dk, "dk"), _pitch(dv, "dv")
-    _check(_packed_backward(ctypes.byref(args), code, _ptr(plan.buffer), plan.sequences, ap, al, _ptr(lse), gp, gl, qp, ql, kp, kl, vp, vl,
-                            _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(dev_status), _stream(stream)))
-    return dq, dk, dv
+    return _result(_elsa_host.packed_attention_backward(q, k, v, plan.buffer, plan.rows, plan.sequences, plan.full, heads,
+                                                        heads if kv_heads is None else kv_heads, causal, scale, da, a, lse, dq, dk, dv, workspace,
+                                                        dev_status, _handle(stream)))
 
 
 def pad_score_table(t):

@@ -30,9 +30,13 @@ constexpr int kRing = 4;                 // tiles of them on their way
 
 template <int kD>
 struct BackwardShape {
-    static constexpr int kThreads = 2 * 128 + 64;
+    static constexpr int kGroups = kD > 64 ? 2 : 1;                  // stages of S and T, each with four warps
+    static constexpr int kThreads = kGroups * 128 + 64;
+    static constexpr int kPerSm = kD > 64 ? 1 : 2;
+    static constexpr int kTmemCols = 512 / kPerSm;
     static constexpr int kKeptBytes = TileShape<kD>::bytes(128), kWalkBytes = TileShape<kD>::bytes(kWalk);
-    static constexpr int kAcc1 = 256, kAcc2 = 256 + kD;              // tensor-memory columns; stage g: S at 128 g, T at 128 g + 64
+    static constexpr int kAcc1 = 128 * kGroups, kAcc2 = kAcc1 + kD;  // tensor-memory columns; stage g: S at 128 g, T at 128 g + 64
+    static_assert(kAcc2 + kD <= kTmemCols, "tensor memory");
     static constexpr int kVectorBytes = 2 * kWalk * 4;               // -lse log2(e), -delta
     static constexpr int kSmemBytes = 2 * kKeptBytes + kRing * (2 * kWalkBytes + kVectorBytes) + 1024 /* delta of the kept rows */ +
                                       1024 /* alignment */ + 256 /* barriers */;
@@ -69,7 +73,7 @@ __device__ __forceinline__ void copies_arrive(uint32_t bar)
 }
 
 template <bool kBf16, int kD, bool kKeys>
-__global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attention_backward_kernel(const __grid_constant__ BackwardParams p)
+__global__ void __launch_bounds__(BackwardShape<kD>::kThreads, BackwardShape<kD>::kPerSm) packed_attention_backward_kernel(const __grid_constant__ BackwardParams p)
 {
     using B = BackwardShape<kD>;
     pdl_wait_for_predecessors();
@@ -96,7 +100,7 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
     static_assert(8 * kBars + 16 <= 256, "barriers");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr int kTmaWarp = 8, kMmaWarp = 9;
+    constexpr int kGroups = B::kGroups, kTmaWarp = 4 * kGroups, kMmaWarp = kTmaWarp + 1;
     // walked tiles: keys from the sequence's start (causal: up to the last kept row); queries to its end (causal: from the first kept row)
     const int walk_from = kKeys && p.causal ? tile.first / kWalk : 0;
     const int walk_end = !kKeys && p.causal && tile.first + 128 < tile.len ? tile.first + 128 : tile.len;
@@ -109,7 +113,7 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
                 mbar_init(bar(kYFull, s), kKeys ? 33 : 1);
                 mbar_init(bar(kYEmpty, s), 1);
             }
-            for (int g = 0; g < 2; ++g) {
+            for (int g = 0; g < kGroups; ++g) {
                 mbar_init(bar(kSFull, g), 1);
                 mbar_init(bar(kPFull, g), 4);
             }
@@ -118,7 +122,7 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
         __syncwarp();
-        tmem_alloc(tmem_holder_addr, 512);
+        tmem_alloc(tmem_holder_addr, B::kTmemCols);
     }
     tc_fence_before();
     __syncthreads();
@@ -174,50 +178,74 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
         const uint32_t x1_desc = Desc::k_major(uniform(smem_base)), x2_desc = x1_desc + (uint32_t)(B::kKeptBytes >> 4);
         const uint32_t y1_rows = Desc::k_major(uniform(y1_smem(0))), y1_cols = Desc::template mn_major<kWalk>(uniform(y1_smem(0)));
         constexpr uint32_t kY2 = (uint32_t)(B::kWalkBytes >> 4);
-        int left = first_left, t = 0, left_before = 0;               // rows of the sequence from this tile's first on; the tile before
-        wait(bar(kXFull, 0), 0, 81);
-        for (int it = 0; ok && it <= tiles; ++it) {
-            if (it < tiles) {
-                const int s = it % kRing, g = it & 1;
-                if (!wait(bar(kYFull, s), it / kRing, 82)) break;
-                if (left < kWalk && (left & 15) != 0) {
-                    zero_rows<kD, kWalk>(y1_smem(s), left, (left + 15) & ~15, lane);
-                    zero_rows<kD, kWalk>(y2_smem(s), left, (left + 15) & ~15, lane);
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                }
-                tc_fence_after();
-                const uint32_t t_s = tmem_u + (uint32_t)(128 * g), y_at = y1_rows + (uint32_t)(s * 2) * kY2;
+        // The loops are unrolled over the ring, so that addresses, barriers and their parities are constants: while this warp works something
+        // out the tensor core idles.  S and T of a tile are issued kGroups - 1 tiles ahead of the sums.
+        auto scores = [&](int s) {
+            const uint32_t t_s = tmem_u + (uint32_t)(128 * (s % kGroups)), y_at = y1_rows + (uint32_t)(s * 2) * kY2;
 #pragma unroll
-                for (int k = 0; k < kD / 16; ++k)
-                    umma_f16_if(t_s, Desc::of(x1_desc + Desc::k_step(128, k)), Desc::of(y_at + Desc::k_step(kWalk, k)), p.idesc_s, (uint32_t)(k != 0), elected);
+            for (int k = 0; k < kD / 16; ++k)
+                umma_f16_if(t_s, Desc::of(x1_desc + Desc::k_step(128, k)), Desc::of(y_at + Desc::k_step(kWalk, k)), p.idesc_s, (uint32_t)(k != 0), elected);
 #pragma unroll
-                for (int k = 0; k < kD / 16; ++k)
-                    umma_f16_if(t_s + 64, Desc::of(x2_desc + Desc::k_step(128, k)), Desc::of(y_at + kY2 + Desc::k_step(kWalk, k)), p.idesc_s, (uint32_t)(k != 0), elected);
-                umma_commit_if(bar(kSFull, g), elected);
-            }
-            if (it > 0) {
-                const int m = it - 1, s = m % kRing, g = m & 1;
-                if (!wait(bar(kPFull, g), m >> 1, 83)) break;
-                tc_fence_after();
-                const int steps = left_before >= kWalk ? kWalk / 16 : (left_before + 15) / 16;
-                const uint32_t t_s = tmem_u + (uint32_t)(128 * g), y_at = y1_cols + (uint32_t)(s * 2) * kY2;
+            for (int k = 0; k < kD / 16; ++k)
+                umma_f16_if(t_s + 64, Desc::of(x2_desc + Desc::k_step(128, k)), Desc::of(y_at + kY2 + Desc::k_step(kWalk, k)), p.idesc_s, (uint32_t)(k != 0), elected);
+            umma_commit_if(bar(kSFull, s % kGroups), elected);
+        };
+        auto sums = [&](int s, bool first, int steps) {
+            const uint32_t t_s = tmem_u + (uint32_t)(128 * (s % kGroups)), y_at = y1_cols + (uint32_t)(s * 2) * kY2;
+            auto p_step = [&](int k) {
+                umma_f16_ts_if(tmem_u + B::kAcc1, t_s + (uint32_t)(8 * k), Desc::of(y_at + kY2 + (uint32_t)k * Desc::kRowsStep), p.idesc_acc,
+                               k != 0 ? 1u : first ? 0u : 1u, elected);
+            };
+            auto ds_step = [&](int k) {
+                umma_f16_ts_if(tmem_u + B::kAcc2, t_s + (uint32_t)(64 + 8 * k), Desc::of(y_at + (uint32_t)k * Desc::kRowsStep), p.idesc_acc,
+                               k != 0 ? 1u : first ? 0u : 1u, elected);
+            };
+            if (steps >= kWalk / 16) {
                 if constexpr (kKeys) {
 #pragma unroll
-                    for (int k = 0; k < kWalk / 16; ++k)
-                        umma_f16_ts_if(tmem_u + B::kAcc1, t_s + (uint32_t)(8 * k), Desc::of(y_at + kY2 + k * Desc::kRowsStep), p.idesc_acc,
-                                       (uint32_t)(m != 0 || k != 0), k < steps ? elected : 0u);
+                    for (int k = 0; k < kWalk / 16; ++k) p_step(k);
                 }
 #pragma unroll
-                for (int k = 0; k < kWalk / 16; ++k)
-                    umma_f16_ts_if(tmem_u + B::kAcc2, t_s + (uint32_t)(64 + 8 * k), Desc::of(y_at + k * Desc::kRowsStep), p.idesc_acc,
-                                   (uint32_t)(m != 0 || k != 0), k < steps ? elected : 0u);
-                umma_commit_if(bar(kYEmpty, s), elected);
-                if (m == tiles - 1) umma_commit_if(bar(kDone, 0), elected);
+                for (int k = 0; k < kWalk / 16; ++k) ds_step(k);
+            } else {
+#pragma unroll 1
+                for (int k = 0; k < steps; ++k) {
+                    if constexpr (kKeys) p_step(k);
+                    ds_step(k);
+                }
             }
-            left_before = left;
-            left -= kWalk;
-            if (++t == tiles_a_head) { t = 0; left = first_left; }
+            umma_commit_if(bar(kYEmpty, s), elected);
+        };
+        int left = first_left, t = 0, left_before = 0;               // rows of the sequence from a tile's first on; those of the tile before
+        wait(bar(kXFull, 0), 0, 81);
+        for (int it0 = 0, round = 0; ok && it0 < tiles + kGroups - 1; it0 += kRing, ++round) {
+#pragma unroll
+            for (int s = 0; s < kRing; ++s) {
+                const int it = it0 + s;
+                if (!ok || it >= tiles + kGroups - 1) break;
+                if (it < tiles) {
+                    if (!wait(bar(kYFull, s), round, 82)) break;
+                    if (left < kWalk && (left & 15) != 0) {
+                        zero_rows<kD, kWalk>(y1_smem(s), left, (left + 15) & ~15, lane);
+                        zero_rows<kD, kWalk>(y2_smem(s), left, (left + 15) & ~15, lane);
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                    }
+                    tc_fence_after();
+                    scores(s);
+                }
+                constexpr int kBehind = kGroups - 1;
+                if (it >= kBehind) {
+                    const int m = it - kBehind, ms = (s + kRing - kBehind) % kRing;            // the tile whose sums are due, and its stage
+                    if (!wait(bar(kPFull, ms % kGroups), ms / kGroups, 83)) break;             // a round of the ring has an even number of a group's tiles
+                    tc_fence_after();
+                    sums(ms, m == 0, ((kBehind ? left_before : left) + 15) >> 4);
+                    if (m == tiles - 1) umma_commit_if(bar(kDone, 0), elected);
+                }
+                left_before = left;
+                left -= kWalk;
+                if (++t == tiles_a_head) { t = 0; left = first_left; }
+            }
         }
         __syncwarp();
     } else {
@@ -228,14 +256,15 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
         const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16);
         float minus_lse = 0.f, minus_delta = 0.f;
         if constexpr (!kKeys) {
-            // delta: half a row by each group
+            // delta: a part of the row by each group
             const size_t at = (size_t)head * (size_t)p.rows + (size_t)(tile.begin + row);
+            constexpr int kPart = kD / kGroups;
             float part = 0.f;
             if (exists) {
-                const uint4* a4 = reinterpret_cast<const uint4*>(p.a + (long long)(tile.begin + row) * p.a_pitch + head * kD + g * (kD / 2));
-                const uint4* d4 = reinterpret_cast<const uint4*>(p.da + (long long)(tile.begin + row) * p.da_pitch + head * kD + g * (kD / 2));
+                const uint4* a4 = reinterpret_cast<const uint4*>(p.a + (long long)(tile.begin + row) * p.a_pitch + head * kD + g * kPart);
+                const uint4* d4 = reinterpret_cast<const uint4*>(p.da + (long long)(tile.begin + row) * p.da_pitch + head * kD + g * kPart);
 #pragma unroll
-                for (int v = 0; v < kD / 16; ++v) {
+                for (int v = 0; v < kPart / 8; ++v) {
                     const uint4 x = __ldg(a4 + v), y = __ldg(d4 + v);
                     const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
@@ -246,26 +275,29 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
                 }
                 minus_lse = -1.4426950408889634f * __ldg(p.lse + at);
             }
-            const uint32_t mine = kept_delta + (uint32_t)(4 * (quarter * 32 + lane));
-            asm volatile("st.shared.f32 [%0], %1;" ::"r"(mine + (uint32_t)(512 * g)), "f"(part) : "memory");
-            asm volatile("bar.sync 1, 256;" ::: "memory");
-            float first, second;
-            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(first) : "r"(mine) : "memory");
-            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(second) : "r"(mine + 512u) : "memory");
-            minus_delta = -(first + second);
+            if constexpr (kGroups > 1) {
+                const uint32_t mine = kept_delta + (uint32_t)(4 * (quarter * 32 + lane));
+                asm volatile("st.shared.f32 [%0], %1;" ::"r"(mine + (uint32_t)(512 * g)), "f"(part) : "memory");
+                asm volatile("bar.sync 1, %0;" ::"n"(128 * kGroups) : "memory");
+                float first, second;
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(first) : "r"(mine) : "memory");
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(second) : "r"(mine + 512u) : "memory");
+                part = first + second;
+            }
+            minus_delta = -part;
             if (g == 0 && exists) {
                 p.minus_lse[at] = minus_lse;
-                p.minus_delta[at] = minus_delta;
+                if (n > 1) p.minus_delta[at] = minus_delta;
             }
         }
         const uint64_t scale2 = f32x2(p.scale_log2, p.scale_log2);
-        for (int it = g; it < n; it += 2) {
+        for (int it = g; it < n; it += kGroups) {
             const int s = it % kRing;
             const int walked = (walk_from + it % per_head) * kWalk;                    // first walked row, in the sequence
             if constexpr (kKeys) {
                 if (!wait(bar(kYFull, s), it / kRing, 84)) break;                      // lse and delta
             }
-            if (!wait(bar(kSFull, g), it >> 1, 85)) break;
+            if (!wait(bar(kSFull, g), it / kGroups, 85)) break;
             tc_fence_after();
             if (row0 < tile.len) {
                 // columns [lo, hi) take part.  Walked queries behind the sequence's end need no test: their rows of q and da are zero,
@@ -274,6 +306,25 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
                 const int hi = kKeys ? kWalk : (p.causal && row + 1 < tile.len ? row + 1 : tile.len) - walked;
                 const bool whole = __all_sync(0xFFFFFFFFu, lo <= 0 && hi >= kWalk);
                 const uint32_t vec = vectors + (uint32_t)(s * B::kVectorBytes);
+                // With all keys of a row in one tile delta is the sum of p T, exact: from the rounded a it is off by half a step of a, as much as
+                // ds itself where there are few keys (with 64 of them an eighth of that).
+                if (!kKeys && n == 1) {
+                    float sum = 0.f;
+#pragma unroll 1
+                    for (int c = 0; c < kWalk; c += 16) {
+                        uint32_t rs[16], rt[16];
+                        tmem_ld_32x32b_x16(t_lane + (uint32_t)(128 * g + c), rs);
+                        tmem_ld_32x32b_x16(t_lane + (uint32_t)(128 * g + 64 + c), rt);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const float e = exp2_approx(fmaf(__uint_as_float(rs[i]), p.scale_log2, minus_lse));
+                            if (c + i < hi) sum = fmaf(e, __uint_as_float(rt[i]), sum);
+                        }
+                    }
+                    minus_delta = -sum;
+                    if (exists) p.minus_delta[(size_t)head * (size_t)p.rows + (size_t)(tile.begin + row)] = minus_delta;
+                }
                 auto unit = [&](auto masked, int u) {
                     uint32_t rs[32], rt[32];
                     tmem_ld_32x32b_x32(t_lane + (uint32_t)(128 * g + 32 * u), rs);
@@ -326,18 +377,21 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
             const uint32_t stage = y1_smem(0) + (uint32_t)(4096 * warp);
             const long long first = tile.begin + row0;
             if constexpr (kKeys) {
-                uint16_t* dst = (g == 0 ? p.out1 + first * p.out1_pitch : p.out2 + first * p.out2_pitch) + head * kD;
                 constexpr int kCols = TileShape<kD>::kCols;
 #pragma unroll
-                for (int c = 0; c < kD; c += kCols)
-                    store_rows<kBf16, kCols>(t_lane + (uint32_t)((g == 0 ? B::kAcc1 : B::kAcc2) + c), g == 0 ? 1.f : p.scale, stage, dst + c,
-                                             g == 0 ? p.out1_pitch : p.out2_pitch, tile.len - row0, lane);
+                for (int o = 0; o < 2; ++o) {                        // dv, then dk; one by each of two groups
+                    if (kGroups > 1 && o != g) continue;
+                    uint16_t* dst = (o == 0 ? p.out1 + first * p.out1_pitch : p.out2 + first * p.out2_pitch) + head * kD;
+#pragma unroll
+                    for (int c = 0; c < kD; c += kCols)
+                        store_rows<kBf16, kCols>(t_lane + (uint32_t)((o == 0 ? B::kAcc1 : B::kAcc2) + c), o == 0 ? 1.f : p.scale, stage, dst + c,
+                                                 o == 0 ? p.out1_pitch : p.out2_pitch, tile.len - row0, lane);
+                }
             } else {
-                // half the columns by each group; heads of 32 columns by the first alone
-                constexpr int kCols = kD == 128 ? 64 : 32;
-                if (kCols * g < kD)
-                    store_rows<kBf16, kCols>(t_lane + (uint32_t)(B::kAcc2 + kCols * g), p.scale, stage, p.out2 + first * p.out2_pitch + head * kD + kCols * g,
-                                             p.out2_pitch, tile.len - row0, lane);
+                // a part of the columns by each group
+                constexpr int kCols = kD / kGroups;
+                store_rows<kBf16, kCols>(t_lane + (uint32_t)(B::kAcc2 + kCols * g), p.scale, stage, p.out2 + first * p.out2_pitch + head * kD + kCols * g,
+                                         p.out2_pitch, tile.len - row0, lane);
             }
         }
     }
@@ -346,7 +400,7 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
     __syncthreads();
     if (warp == kMmaWarp) {
         tc_fence_after();
-        tmem_dealloc(tmem_base, 512);
+        tmem_dealloc(tmem_base, B::kTmemCols);
     }
 }
 
@@ -354,7 +408,7 @@ template <bool kBf16, int kD, bool kKeys>
 elsa_status launch(const BackwardParams& p, cudaStream_t stream, const DeviceInfo& dev)
 {
     using B = BackwardShape<kD>;
-    static_assert(2 * kRing * B::kWalkBytes >= 8 * 4096, "staging room");
+    static_assert(2 * kRing * B::kWalkBytes >= 4 * B::kGroups * 4096, "staging room");
     auto kernel = packed_attention_backward_kernel<kBf16, kD, kKeys>;
     static std::atomic<bool> attr_set[64];
     const int slot = dev.device & 63;
