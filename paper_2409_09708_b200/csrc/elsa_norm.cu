@@ -13,18 +13,28 @@ namespace elsa {
 namespace {
 
 constexpr int kMaxNormDim = 16384;      // 16 warps of 32 lanes with four vectors of eight
-constexpr int kMaxParts = 592;          // rows of partial sums: at most four CTAs on each of 148 SMs
 
-template <int kLanes, int kRowWarps>
+// kLeast: threads of a CTA where a row needs no more (256 forward, 128 for the gradient, whose registers allow CTAs of that size only in
+// halves: 1384 columns 14.5 us forward, 16.2 with 128)
+template <int kLanes, int kRowWarps, int kLeast>
 struct Group {
-    static constexpr int kThreads = kRowWarps > 8 ? kRowWarps * 32 : 256;
+    static constexpr int kThreads = kRowWarps * 32 > kLeast ? kRowWarps * 32 : kLeast;
     static constexpr int kRowLanes = kRowWarps > 1 ? kRowWarps * 32 : kLanes;   // lanes of a row
     static constexpr int kGroups = kThreads / kRowLanes;                        // rows side by side in a CTA
 };
 
+// CTAs of the gradient kernel on an SM: what its registers allow (two sums and three tensors' vectors of a row for each vector of a
+// lane).  HBM bounds it: 50432 x 768 with a residual 60 us, 5.2 TB/s, 401408 x 128 71 us, 5.7 (one CTA of
+// eight warps whatever the width: 63 and 109).
+constexpr int backward_per_sm(int row_lanes, int vpl)
+{
+    const int warps = vpl == 1 ? 28 : vpl == 2 ? 16 : vpl == 3 ? 8 : 8, cta_warps = row_lanes > 128 ? row_lanes / 32 : 4;
+    return warps / cta_warps < 1 ? 1 : warps / cta_warps;
+}
+
 // Sums of a row's lanes, the same bits in each of them.  Row groups of several warps meet at a barrier of their own; two buffers
 // in turn, so that one barrier a sum is enough.
-template <int kLanes, int kRowWarps>
+template <class G, int kLanes, int kRowWarps>
 __device__ __forceinline__ float2 row_sums(float2 v, float2* buffer, int& turn)
 {
 #pragma unroll
@@ -34,7 +44,7 @@ __device__ __forceinline__ float2 row_sums(float2 v, float2* buffer, int& turn)
     }
     if constexpr (kRowWarps > 1) {
         const int warp = threadIdx.x >> 5, group = warp / kRowWarps;
-        float2* row = buffer + (turn * Group<kLanes, kRowWarps>::kGroups + group) * kRowWarps;
+        float2* row = buffer + (turn * G::kGroups + group) * kRowWarps;
         turn ^= 1;
         if ((threadIdx.x & 31) == 0) row[warp % kRowWarps] = v;
         asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(kRowWarps * 32) : "memory");
@@ -47,11 +57,11 @@ __device__ __forceinline__ float2 row_sums(float2 v, float2* buffer, int& turn)
 
 // Any width up to kMaxNormDim; the model widths have layer_norm_rows_kernel.
 template <bool kBf16, bool kAdd, int kLanes, int kRowWarps, int kVpl>
-__global__ void __launch_bounds__(Group<kLanes, kRowWarps>::kThreads)
+__global__ void __launch_bounds__(Group<kLanes, kRowWarps, 256>::kThreads)
 layer_norm_columns_kernel(const uint16_t* A, const uint16_t* R, uint16_t* S, const uint16_t* __restrict__ gain,
                           const uint16_t* __restrict__ beta, uint16_t* Y, float2* stats, int rows, int dim, float eps)
 {
-    using G = Group<kLanes, kRowWarps>;
+    using G = Group<kLanes, kRowWarps, 256>;
     __shared__ float2 sums[2 * G::kGroups * kRowWarps];
     pdl_wait_for_predecessors();
     pdl_release_successors();
@@ -95,7 +105,7 @@ layer_norm_columns_kernel(const uint16_t* A, const uint16_t* R, uint16_t* S, con
         }
         load(row + stride);
         // a division, so that a constant row has its value as the mean, whatever the width
-        const float mean = row_sums<kLanes, kRowWarps>(t, sums, turn).x / (float)dim;
+        const float mean = row_sums<G, kLanes, kRowWarps>(t, sums, turn).x / (float)dim;
         t.x = 0.f;
 #pragma unroll
         for (int c = 0; c < kVpl; ++c) {
@@ -106,7 +116,7 @@ layer_norm_columns_kernel(const uint16_t* A, const uint16_t* R, uint16_t* S, con
                 t.x += f[c][e] * f[c][e];
             }
         }
-        const float rstd = 1.0f / sqrtf(row_sums<kLanes, kRowWarps>(t, sums, turn).x / (float)dim + eps);
+        const float rstd = 1.0f / sqrtf(row_sums<G, kLanes, kRowWarps>(t, sums, turn).x / (float)dim + eps);
         if (row >= rows) continue;
         if (stats != nullptr && sub == 0) stats[row] = make_float2(mean, rstd);
 #pragma unroll
@@ -125,11 +135,11 @@ layer_norm_columns_kernel(const uint16_t* A, const uint16_t* R, uint16_t* S, con
 
 // dX may be dY's or dS's own buffer: a lane reads its vectors of a row before it writes them, and no one else touches them.
 template <bool kBf16, bool kAdd, int kLanes, int kRowWarps, int kVpl>
-__global__ void __launch_bounds__(Group<kLanes, kRowWarps>::kThreads)
+__global__ void __launch_bounds__(Group<kLanes, kRowWarps, 128>::kThreads, backward_per_sm(Group<kLanes, kRowWarps, 128>::kRowLanes, kVpl))
 layer_norm_backward_kernel(const uint16_t* dY, const uint16_t* __restrict__ S, const float2* __restrict__ stats,
                            const uint16_t* __restrict__ gain, const uint16_t* dS, uint16_t* dX, float* partial, int rows, int dim)
 {
-    using G = Group<kLanes, kRowWarps>;
+    using G = Group<kLanes, kRowWarps, 128>;
     __shared__ float2 sums[2 * G::kGroups * kRowWarps];
     extern __shared__ float4 column_sums[];                  // [2][dim], with several row groups
     float* columns = reinterpret_cast<float*>(column_sums);
@@ -141,14 +151,19 @@ layer_norm_backward_kernel(const uint16_t* dY, const uint16_t* __restrict__ S, c
     const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
     uint4 x[kVpl], d[kVpl], r[kAdd ? kVpl : 1], gn[kVpl];
     float2 st = make_float2(0.f, 0.f);
-    float dgain[kVpl][8], dbias[kVpl][8];
+    // rows of more than 8192 values: 512 threads leave no registers for the sums, and one row group has the shared memory for itself
+    constexpr bool kSharedSums = kRowWarps > 8;
+    float dgain[kSharedSums ? 1 : kVpl][8], dbias[kSharedSums ? 1 : kVpl][8];
     int turn = 0;
 #pragma unroll
     for (int c = 0; c < kVpl; ++c) {
         const int v = sub + G::kRowLanes * c;
         gn[c] = v < vecs ? __ldg(reinterpret_cast<const uint4*>(gain) + v) : zero;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) dgain[c][e] = dbias[c][e] = 0.f;
+        for (int e = 0; e < 8; ++e) {
+            if constexpr (!kSharedSums) dgain[c][e] = dbias[c][e] = 0.f;
+            else if (partial != nullptr && v < vecs) columns[8 * v + e] = columns[dim + 8 * v + e] = 0.f;
+        }
     }
     auto load = [&](int row) {
         st = row < rows ? __ldg(stats + row) : make_float2(0.f, 0.f);
@@ -178,19 +193,39 @@ layer_norm_backward_kernel(const uint16_t* dY, const uint16_t* __restrict__ S, c
             unpack8<kBf16>(d[c], g[c]);
             unpack8<kBf16>(gn[c], gv);
             if constexpr (kAdd) rr[c] = r[c];
+            const int v = sub + G::kRowLanes * c;
+            float4* sum4 = reinterpret_cast<float4*>(columns + 8 * v);
+            float had[2][8];
+            if constexpr (kSharedSums) {
+                if (partial != nullptr && v < vecs) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) reinterpret_cast<float4*>(had[q >> 1])[q & 1] = sum4[(q >> 1) * (dim >> 2) + (q & 1)];
+                }
+            }
             // columns past the row's end and rows past the last have dy = 0 and a mean and rstd that are finite: they add nothing
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 xhat[c][e] = (xhat[c][e] - st.x) * rstd;
-                dgain[c][e] += g[c][e] * xhat[c][e];
-                dbias[c][e] += g[c][e];
+                if constexpr (kSharedSums) {
+                    had[0][e] += g[c][e] * xhat[c][e];
+                    had[1][e] += g[c][e];
+                } else {
+                    dgain[c][e] += g[c][e] * xhat[c][e];
+                    dbias[c][e] += g[c][e];
+                }
                 g[c][e] *= gv[e];
                 t.x += g[c][e];
                 t.y += g[c][e] * xhat[c][e];
             }
+            if constexpr (kSharedSums) {
+                if (partial != nullptr && v < vecs) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) sum4[(q >> 1) * (dim >> 2) + (q & 1)] = reinterpret_cast<float4*>(had[q >> 1])[q & 1];
+                }
+            }
         }
         load(row + stride);
-        const float2 m = row_sums<kLanes, kRowWarps>(t, sums, turn);
+        const float2 m = row_sums<G, kLanes, kRowWarps>(t, sums, turn);
         if (dX == nullptr || row >= rows) continue;
         const float c1 = m.x * inv_dim, c2 = m.y * inv_dim;
 #pragma unroll
@@ -205,6 +240,15 @@ layer_norm_backward_kernel(const uint16_t* dY, const uint16_t* __restrict__ S, c
         }
     }
     if (partial == nullptr) return;
+    if constexpr (kSharedSums) {
+        float4* out = reinterpret_cast<float4*>(partial + (size_t)blockIdx.x * (size_t)(2 * dim));
+        for (int c = 0; c < kVpl; ++c) {
+            const int v = sub + G::kRowLanes * c;
+            if (v >= vecs) continue;
+            for (int q = 0; q < 4; ++q) out[(q >> 1) * (dim >> 2) + 2 * v + (q & 1)] = column_sums[(q >> 1) * (dim >> 2) + 2 * v + (q & 1)];
+        }
+        return;
+    } else {
     // the row groups of the CTA, one after another in a fixed order: columns [2][dim]
 #pragma unroll 1
     for (int k = 0; k < G::kGroups; ++k) {
@@ -237,14 +281,16 @@ layer_norm_backward_kernel(const uint16_t* dY, const uint16_t* __restrict__ S, c
         }
         if (G::kGroups > 1) __syncthreads();
     }
+    }
 }
 
-// out[c] = round16(sum over parts of partial[part][c]): 32 columns a block, the parts over its eight warps.
+// out[c] = round16(sum over parts of partial[part][c]): 32 columns a block, the parts over its warps.
+constexpr int kSumWarps = 32;
 template <bool kBf16>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kSumWarps * 32)
 norm_sums_kernel(const float* __restrict__ partial, int parts, int dim, uint16_t* dgain, uint16_t* dbias)
 {
-    __shared__ float sums[8][32];
+    __shared__ float sums[kSumWarps][33];
     pdl_wait_for_predecessors();
     pdl_release_successors();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -252,20 +298,24 @@ norm_sums_kernel(const float* __restrict__ partial, int parts, int dim, uint16_t
     float t[4] = {0.f, 0.f, 0.f, 0.f};
     if (col < 2 * dim) {
         int p = warp;
-        for (; p + 24 < parts; p += 32) {
+        for (; p + 3 * kSumWarps < parts; p += 4 * kSumWarps) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) t[i] += __ldg(partial + (size_t)(p + 8 * i) * (size_t)(2 * dim) + col);
+            for (int i = 0; i < 4; ++i) t[i] += __ldg(partial + (size_t)(p + kSumWarps * i) * (size_t)(2 * dim) + col);
         }
-        for (; p < parts; p += 8) t[0] += __ldg(partial + (size_t)p * (size_t)(2 * dim) + col);
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (p + kSumWarps * i < parts) t[i] += __ldg(partial + (size_t)(p + kSumWarps * i) * (size_t)(2 * dim) + col);
     }
     sums[warp][lane] = (t[0] + t[1]) + (t[2] + t[3]);
     __syncthreads();
-    if (warp == 0 && col < 2 * dim) {
-        float v = sums[0][lane];
+    // a column to a warp, its parts to the lanes
+    float v = sums[lane][warp];
 #pragma unroll
-        for (int w = 1; w < 8; ++w) v += sums[w][lane];
-        uint16_t* out = col < dim ? dgain : dbias;
-        if (out != nullptr) out[col < dim ? col : col - dim] = (uint16_t)(pack2<kBf16>(v, 0.f) & 0xffffu);
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    const int out_col = blockIdx.x * 32 + warp;
+    if (lane == 0 && out_col < 2 * dim) {
+        uint16_t* out = out_col < dim ? dgain : dbias;
+        if (out != nullptr) out[out_col < dim ? out_col : out_col - dim] = (uint16_t)(pack2<kBf16>(v, 0.f) & 0xffffu);
     }
 }
 
@@ -281,6 +331,13 @@ RowShape row_shape(int dim)
         for (int vpl = 1; vpl <= 4; ++vpl)
             if (lanes * vpl >= vecs && lanes * vpl <= best.lanes * best.vpl) best = {lanes, vpl};
     return best;
+}
+
+// Rows of partial sums: one of each CTA that the 148 SMs of the device hold.
+int max_parts(int dim)
+{
+    const RowShape shape = row_shape(dim);
+    return 148 * backward_per_sm(shape.lanes, shape.vpl);
 }
 
 #define ELSA_NORM_VPL(MACRO, LANES, WARPS)                                     \
@@ -310,8 +367,8 @@ cudaError_t forward(const RowShape& shape, const uint16_t* A, const uint16_t* R,
     cudaError_t e = cudaSuccess;
 #define ELSA_NORM_FORWARD(LANES, WARPS, VPL)                                                                                   \
     do {                                                                                                                       \
-        using G = Group<LANES, WARPS>;                                                                                         \
-        const int blocks = (rows - 1) / G::kGroups + 1, most = dev.sm_count * 8 * 256 / G::kThreads;                           \
+        using G = Group<LANES, WARPS, 256>;                                                                                    \
+        const int blocks = (rows - 1) / G::kGroups + 1, most = dev.sm_count * 2048 / G::kThreads;                           \
         e = launch_pdl(layer_norm_columns_kernel<kBf16, kAdd, LANES, WARPS, VPL>, dim3((unsigned)(blocks < most ? blocks : most)), \
                        dim3(G::kThreads), 0, stream, 1, A, R, S, gain, beta, Y, stats, rows, dim, eps);                        \
     } while (0)
@@ -328,13 +385,14 @@ cudaError_t backward(const RowShape& shape, const uint16_t* dY, const uint16_t* 
     cudaError_t e = cudaSuccess;
 #define ELSA_NORM_BACKWARD(LANES, WARPS, VPL)                                                                                  \
     do {                                                                                                                       \
-        using G = Group<LANES, WARPS>;                                                                                         \
+        using G = Group<LANES, WARPS, 128>;                                                                                    \
         auto kernel = layer_norm_backward_kernel<kBf16, kAdd, LANES, WARPS, VPL>;                                              \
-        const size_t smem = partial != nullptr && G::kGroups > 1 ? (size_t)dim * 8 : 0;   /* at most 4096 columns: 32 KB */    \
-        const int per_sm = G::kThreads > 256 ? 1 : VPL >= 3 ? 1 : 2;                                                           \
-        const int blocks = (rows - 1) / G::kGroups + 1, resident = dev.sm_count * per_sm;                                      \
-        const int most = resident < kMaxParts ? resident : kMaxParts;                                                          \
+        constexpr bool kShared = WARPS > 8;                                                                                    \
+        const size_t smem = partial != nullptr && (G::kGroups > 1 || kShared) ? (size_t)dim * 8 : 0;   /* up to 32 KB, or 128 */ \
+        const int blocks = (rows - 1) / G::kGroups + 1, most = max_parts(dim);                                                 \
         *parts = blocks < most ? blocks : most;                                                                                \
+        if (kShared) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * kMaxNormDim * (int)sizeof(float)); \
+        if (e == cudaSuccess)                                                                                                  \
         e = launch_pdl(kernel, dim3((unsigned)*parts), dim3(G::kThreads), smem, stream, 1, dY, S, stats, gain, dS, dX, partial, rows, dim); \
     } while (0)
     ELSA_NORM_SHAPES(ELSA_NORM_BACKWARD);
@@ -368,7 +426,7 @@ elsa_status launch_layer_norm_columns(const uint16_t* A, const uint16_t* R, uint
 
 size_t layer_norm_backward_workspace(int rows, int dim)
 {
-    const size_t parts = (size_t)(rows < kMaxParts ? rows : kMaxParts);
+    const size_t parts = (size_t)(rows < max_parts(dim) ? rows : max_parts(dim));
     return parts * (size_t)dim * 2 * sizeof(float);
 }
 
@@ -397,8 +455,8 @@ elsa_status launch_layer_norm_backward(const uint16_t* dY, const uint16_t* S, co
     }
     ProfileScope scope(ELSA_KERNEL_NORM_BACKWARD, stream);
     const dim3 grid((unsigned)((2 * dim + 31) / 32));
-    if (dtype == ELSA_BF16) e = launch_pdl(norm_sums_kernel<true>, grid, dim3(256), 0, stream, 1, partial, parts, dim, dgain, dbias);
-    else e = launch_pdl(norm_sums_kernel<false>, grid, dim3(256), 0, stream, 1, partial, parts, dim, dgain, dbias);
+    if (dtype == ELSA_BF16) e = launch_pdl(norm_sums_kernel<true>, grid, dim3(kSumWarps * 32), 0, stream, 1, partial, parts, dim, dgain, dbias);
+    else e = launch_pdl(norm_sums_kernel<false>, grid, dim3(kSumWarps * 32), 0, stream, 1, partial, parts, dim, dgain, dbias);
     if (e != cudaSuccess) return fail(ELSA_ERR_CUDA, "norm_sums launch: %s", cudaGetErrorString(e));
     return launched("norm_sums");
 }
