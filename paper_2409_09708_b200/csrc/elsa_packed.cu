@@ -102,8 +102,7 @@ packed_attention_kernel(const __grid_constant__ ForwardParams p)
     const int kv_col = head / p.group * kD;
     bool ok = true;
     auto wait = [&](uint32_t b, int count, uint32_t site) {          // for the count-th completion of a barrier, from 0
-        ok = mbar_wait(b, (uint32_t)(count & 1), abort_flag, p.dev_status, site);
-        ok = __all_sync(0xFFFFFFFFu, ok);
+        ok = packed_wait(b, (uint32_t)(count & 1), abort_flag, p.dev_status, site);
         return ok;
     };
     // Stage j % kStages has V of tile j and K of tile j + 1, which the products of one step ask for; K of tile 0 comes with Q, into the

@@ -90,6 +90,20 @@ struct TileDesc {
     __device__ static __forceinline__ uint64_t of(uint32_t low) { return (uint64_t)kHigh << 32 | low; }
 };
 
+// The warp's bounded wait for a barrier's phase.  The common case, one test that succeeds, is all that stands where it is called; the rest
+// is a function of its own, because the issuing warp's unrolled loop is fetched anew every round and each wait of it in full length
+// (with its clock and its report) made that a good part of a tile's time.
+__device__ __noinline__ bool packed_wait_on(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint32_t* dev_status, uint32_t site)
+{
+    const bool ok = mbar_wait(bar, parity, abort_flag, dev_status, site);
+    return __all_sync(0xFFFFFFFFu, ok);
+}
+__device__ __forceinline__ bool packed_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint32_t* dev_status, uint32_t site)
+{
+    if (__all_sync(0xFFFFFFFFu, mbar_try_wait(bar, parity))) return true;
+    return packed_wait_on(bar, parity, abort_flag, dev_status, site);
+}
+
 // A value that all lanes of the (converged) warp hold, in a form that the compiler knows to be one.
 __device__ __forceinline__ uint32_t uniform(uint32_t v) { return __reduce_or_sync(0xFFFFFFFFu, v); }
 __device__ __forceinline__ int uniform(int v) { return (int)__reduce_or_sync(0xFFFFFFFFu, (unsigned)v); }

@@ -26,14 +26,13 @@ namespace elsa {
 namespace {
 
 constexpr int kWalk = 64;                // walked rows of a tile
-constexpr int kRing = 4;                 // tiles of them on their way
 
 template <int kD>
 struct BackwardShape {
-    static constexpr int kGroups = kD > 64 ? 2 : 1;                  // stages of S and T, each with four warps
+    static constexpr int kGroups = kD > 64 ? 2 : 3;                  // stages of S and T, each with four warps
+    static constexpr int kRing = 2 * kGroups;                        // tiles of walked rows on their way
     static constexpr int kThreads = kGroups * 128 + 64;
-    static constexpr int kPerSm = kD > 64 ? 1 : 2;
-    static constexpr int kTmemCols = 512 / kPerSm;
+    static constexpr int kTmemCols = 512;
     static constexpr int kKeptBytes = TileShape<kD>::bytes(128), kWalkBytes = TileShape<kD>::bytes(kWalk);
     static constexpr int kAcc1 = 128 * kGroups, kAcc2 = kAcc1 + kD;  // tensor-memory columns; stage g: S at 128 g, T at 128 g + 64
     static_assert(kAcc2 + kD <= kTmemCols, "tensor memory");
@@ -73,7 +72,7 @@ __device__ __forceinline__ void copies_arrive(uint32_t bar)
 }
 
 template <bool kBf16, int kD, bool kKeys>
-__global__ void __launch_bounds__(BackwardShape<kD>::kThreads, BackwardShape<kD>::kPerSm) packed_attention_backward_kernel(const __grid_constant__ BackwardParams p)
+__global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attention_backward_kernel(const __grid_constant__ BackwardParams p)
 {
     using B = BackwardShape<kD>;
     pdl_wait_for_predecessors();
@@ -89,10 +88,10 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, BackwardShape<kD>
     const uint32_t x1_smem = smem_base, x2_smem = smem_base + B::kKeptBytes;
     auto y1_smem = [&](int s) { return smem_base + (uint32_t)(2 * B::kKeptBytes + 2 * s * B::kWalkBytes); };
     auto y2_smem = [&](int s) { return y1_smem(s) + (uint32_t)B::kWalkBytes; };
-    const uint32_t vectors = smem_base + (uint32_t)(2 * B::kKeptBytes + 2 * kRing * B::kWalkBytes);
-    const uint32_t kept_delta = vectors + kRing * B::kVectorBytes;                     // [2][128] floats
+    const uint32_t vectors = smem_base + (uint32_t)(2 * B::kKeptBytes + 2 * B::kRing * B::kWalkBytes);
+    const uint32_t kept_delta = vectors + B::kRing * B::kVectorBytes;                     // [2][128] floats
     const uint32_t bars = kept_delta + 1024;
-    enum { kXFull = 0, kYFull = 1, kYEmpty = 1 + kRing, kSFull = 1 + 2 * kRing, kPFull = 3 + 2 * kRing, kDone = 5 + 2 * kRing, kBars };
+    enum { kXFull = 0, kYFull = 1, kYEmpty = kYFull + B::kRing, kSFull = kYEmpty + B::kRing, kPFull = kSFull + B::kGroups, kDone = kPFull + B::kGroups, kBars };
     auto bar = [&](int which, int i) { return bars + (uint32_t)(8 * (which + i)); };
     const uint32_t tmem_holder_addr = bars + 8 * kBars;
     uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(smem_raw + (tmem_holder_addr - smem_u32(smem_raw)));
@@ -100,7 +99,7 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, BackwardShape<kD>
     static_assert(8 * kBars + 16 <= 256, "barriers");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr int kGroups = B::kGroups, kTmaWarp = 4 * kGroups, kMmaWarp = kTmaWarp + 1;
+    constexpr int kGroups = B::kGroups, kRing = B::kRing, kTmaWarp = 4 * kGroups, kMmaWarp = kTmaWarp + 1;
     // walked tiles: keys from the sequence's start (causal: up to the last kept row); queries to its end (causal: from the first kept row)
     const int walk_from = kKeys && p.causal ? tile.first / kWalk : 0;
     const int walk_end = !kKeys && p.causal && tile.first + 128 < tile.len ? tile.first + 128 : tile.len;
@@ -131,8 +130,7 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, BackwardShape<kD>
 
     bool ok = true;
     auto wait = [&](uint32_t b, int count, uint32_t site) {          // for the count-th completion of a barrier, from 0
-        ok = mbar_wait(b, (uint32_t)(count & 1), abort_flag, p.dev_status, site);
-        ok = __all_sync(0xFFFFFFFFu, ok);
+        ok = packed_wait(b, (uint32_t)(count & 1), abort_flag, p.dev_status, site);
         return ok;
     };
     if (warp == kTmaWarp) {
@@ -216,7 +214,8 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, BackwardShape<kD>
             }
             umma_commit_if(bar(kYEmpty, s), elected);
         };
-        int left = first_left, t = 0, left_before = 0;               // rows of the sequence from a tile's first on; those of the tile before
+        // rows of the sequence from a tile's first on: of the tile whose S and T are due, and of the one whose sums are
+        int left = first_left, t = 0, sums_left = first_left, sums_t = 0;
         wait(bar(kXFull, 0), 0, 81);
         for (int it0 = 0, round = 0; ok && it0 < tiles + kGroups - 1; it0 += kRing, ++round) {
 #pragma unroll
@@ -239,10 +238,11 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, BackwardShape<kD>
                     const int m = it - kBehind, ms = (s + kRing - kBehind) % kRing;            // the tile whose sums are due, and its stage
                     if (!wait(bar(kPFull, ms % kGroups), ms / kGroups, 83)) break;             // a round of the ring has an even number of a group's tiles
                     tc_fence_after();
-                    sums(ms, m == 0, ((kBehind ? left_before : left) + 15) >> 4);
+                    sums(ms, m == 0, (sums_left + 15) >> 4);
+                    sums_left -= kWalk;
+                    if (++sums_t == tiles_a_head) { sums_t = 0; sums_left = first_left; }
                     if (m == tiles - 1) umma_commit_if(bar(kDone, 0), elected);
                 }
-                left_before = left;
                 left -= kWalk;
                 if (++t == tiles_a_head) { t = 0; left = first_left; }
             }
@@ -256,11 +256,12 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, BackwardShape<kD>
         const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16);
         float minus_lse = 0.f, minus_delta = 0.f;
         if constexpr (!kKeys) {
-            // delta: a part of the row by each group
+            // delta: half a row by each of two groups
             const size_t at = (size_t)head * (size_t)p.rows + (size_t)(tile.begin + row);
-            constexpr int kPart = kD / kGroups;
+            constexpr int kPart = kD / 2;
             float part = 0.f;
-            if (exists) {
+            if (exists) minus_lse = -1.4426950408889634f * __ldg(p.lse + at);
+            if (exists && g < 2) {
                 const uint4* a4 = reinterpret_cast<const uint4*>(p.a + (long long)(tile.begin + row) * p.a_pitch + head * kD + g * kPart);
                 const uint4* d4 = reinterpret_cast<const uint4*>(p.da + (long long)(tile.begin + row) * p.da_pitch + head * kD + g * kPart);
 #pragma unroll
@@ -273,11 +274,10 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, BackwardShape<kD>
                         part = fmaf(u.x, w.x, fmaf(u.y, w.y, part));
                     }
                 }
-                minus_lse = -1.4426950408889634f * __ldg(p.lse + at);
             }
-            if constexpr (kGroups > 1) {
+            {
                 const uint32_t mine = kept_delta + (uint32_t)(4 * (quarter * 32 + lane));
-                asm volatile("st.shared.f32 [%0], %1;" ::"r"(mine + (uint32_t)(512 * g)), "f"(part) : "memory");
+                if (g < 2) asm volatile("st.shared.f32 [%0], %1;" ::"r"(mine + (uint32_t)(512 * g)), "f"(part) : "memory");
                 asm volatile("bar.sync 1, %0;" ::"n"(128 * kGroups) : "memory");
                 float first, second;
                 asm volatile("ld.shared.f32 %0, [%1];" : "=f"(first) : "r"(mine) : "memory");
@@ -379,8 +379,8 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, BackwardShape<kD>
             if constexpr (kKeys) {
                 constexpr int kCols = TileShape<kD>::kCols;
 #pragma unroll
-                for (int o = 0; o < 2; ++o) {                        // dv, then dk; one by each of two groups
-                    if (kGroups > 1 && o != g) continue;
+                for (int o = 0; o < 2; ++o) {                        // dv by one group, dk by another
+                    if (o != g) continue;
                     uint16_t* dst = (o == 0 ? p.out1 + first * p.out1_pitch : p.out2 + first * p.out2_pitch) + head * kD;
 #pragma unroll
                     for (int c = 0; c < kD; c += kCols)
@@ -388,10 +388,11 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, BackwardShape<kD>
                                                  o == 0 ? p.out1_pitch : p.out2_pitch, tile.len - row0, lane);
                 }
             } else {
-                // a part of the columns by each group
-                constexpr int kCols = kD / kGroups;
-                store_rows<kBf16, kCols>(t_lane + (uint32_t)(B::kAcc2 + kCols * g), p.scale, stage, p.out2 + first * p.out2_pitch + head * kD + kCols * g,
-                                         p.out2_pitch, tile.len - row0, lane);
+                // half the columns by each of two groups; heads of 32 columns by the first alone
+                constexpr int kCols = kD / 2 < 32 ? 32 : kD / 2;
+                if (kCols * g < kD)
+                    store_rows<kBf16, kCols>(t_lane + (uint32_t)(B::kAcc2 + kCols * g), p.scale, stage, p.out2 + first * p.out2_pitch + head * kD + kCols * g,
+                                             p.out2_pitch, tile.len - row0, lane);
             }
         }
     }
@@ -408,7 +409,7 @@ template <bool kBf16, int kD, bool kKeys>
 elsa_status launch(const BackwardParams& p, cudaStream_t stream, const DeviceInfo& dev)
 {
     using B = BackwardShape<kD>;
-    static_assert(2 * kRing * B::kWalkBytes >= 4 * B::kGroups * 4096, "staging room");
+    static_assert(2 * B::kRing * B::kWalkBytes >= 4 * B::kGroups * 4096, "staging room");
     auto kernel = packed_attention_backward_kernel<kBf16, kD, kKeys>;
     static std::atomic<bool> attr_set[64];
     const int slot = dev.device & 63;
