@@ -176,20 +176,22 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
         const uint32_t x1_desc = Desc::k_major(uniform(smem_base)), x2_desc = x1_desc + (uint32_t)(B::kKeptBytes >> 4);
         const uint32_t y1_rows = Desc::k_major(uniform(y1_smem(0))), y1_cols = Desc::template mn_major<kWalk>(uniform(y1_smem(0)));
         constexpr uint32_t kY2 = (uint32_t)(B::kWalkBytes >> 4);
-        // The loops are unrolled over the ring, so that addresses, barriers and their parities are constants: while this warp works something
-        // out the tensor core idles.  S and T of a tile are issued kGroups - 1 tiles ahead of the sums.
-        auto scores = [&](int s) {
-            const uint32_t t_s = tmem_u + (uint32_t)(128 * (s % kGroups)), y_at = y1_rows + (uint32_t)(s * 2) * kY2;
+        // The loop is unrolled over the stages, so that their addresses are constants, and does little else than wait and issue: while this warp
+        // works something out the tensor core idles.  S and T of a tile are issued kGroups - 1 tiles ahead of the sums.  The ring has two
+        // rounds of the stages: y_round is the offset of the one that S and T (the sums) are in, as descriptors count.
+        constexpr uint32_t kRound = (uint32_t)(kGroups * 2) * kY2;
+        auto scores = [&](int g, uint32_t y_round) {
+            const uint32_t t_s = tmem_u + (uint32_t)(128 * g), y_at = y1_rows + y_round + (uint32_t)(g * 2) * kY2;
 #pragma unroll
             for (int k = 0; k < kD / 16; ++k)
                 umma_f16_if(t_s, Desc::of(x1_desc + Desc::k_step(128, k)), Desc::of(y_at + Desc::k_step(kWalk, k)), p.idesc_s, (uint32_t)(k != 0), elected);
 #pragma unroll
             for (int k = 0; k < kD / 16; ++k)
                 umma_f16_if(t_s + 64, Desc::of(x2_desc + Desc::k_step(128, k)), Desc::of(y_at + kY2 + Desc::k_step(kWalk, k)), p.idesc_s, (uint32_t)(k != 0), elected);
-            umma_commit_if(bar(kSFull, s % kGroups), elected);
+            umma_commit_if(bar(kSFull, g), elected);
         };
-        auto sums = [&](int s, bool first, int steps) {
-            const uint32_t t_s = tmem_u + (uint32_t)(128 * (s % kGroups)), y_at = y1_cols + (uint32_t)(s * 2) * kY2;
+        auto sums = [&](int g, uint32_t y_round, bool first, int steps) {
+            const uint32_t t_s = tmem_u + (uint32_t)(128 * g), y_at = y1_cols + y_round + (uint32_t)(g * 2) * kY2;
             auto p_step = [&](int k) {
                 umma_f16_ts_if(tmem_u + B::kAcc1, t_s + (uint32_t)(8 * k), Desc::of(y_at + kY2 + (uint32_t)k * Desc::kRowsStep), p.idesc_acc,
                                k != 0 ? 1u : first ? 0u : 1u, elected);
@@ -198,7 +200,7 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
                 umma_f16_ts_if(tmem_u + B::kAcc2, t_s + (uint32_t)(64 + 8 * k), Desc::of(y_at + (uint32_t)k * Desc::kRowsStep), p.idesc_acc,
                                k != 0 ? 1u : first ? 0u : 1u, elected);
             };
-            if (steps >= kWalk / 16) {
+            if (steps == kWalk / 16) {
                 if constexpr (kKeys) {
 #pragma unroll
                     for (int k = 0; k < kWalk / 16; ++k) p_step(k);
@@ -212,40 +214,53 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
                     ds_step(k);
                 }
             }
-            umma_commit_if(bar(kYEmpty, s), elected);
         };
-        // rows of the sequence from a tile's first on: of the tile whose S and T are due, and of the one whose sums are
-        int left = first_left, t = 0, sums_left = first_left, sums_t = 0;
+        // the last tile of a head's may be ragged: rows of it, and tiles up to it
+        const int last_left = first_left - (tiles_a_head - 1) * kWalk;
+        const int last_steps = last_left >= kWalk ? kWalk / 16 : (last_left + 15) / 16;
+        int to_last = tiles_a_head, sums_to_last = tiles_a_head;
         wait(bar(kXFull, 0), 0, 81);
-        for (int it0 = 0, round = 0; ok && it0 < tiles + kGroups - 1; it0 += kRing, ++round) {
+        uint32_t half = 0, ring_phase = 0;                           // round of the stages, phase of the ring's barriers
+        for (int it0 = 0; ok && it0 < tiles + kGroups - 1; it0 += kGroups) {
+            const uint32_t y_round = half != 0 ? kRound : 0u, y_before = kRound - y_round;
+            const uint32_t round_bars = half != 0 ? 8u * kGroups : 0u, before_bars = 8u * kGroups - round_bars;
 #pragma unroll
-            for (int s = 0; s < kRing; ++s) {
-                const int it = it0 + s;
-                if (!ok || it >= tiles + kGroups - 1) break;
+            for (int g = 0; g < kGroups; ++g) {
+                const int it = it0 + g;
                 if (it < tiles) {
-                    if (!wait(bar(kYFull, s), round, 82)) break;
-                    if (left < kWalk && (left & 15) != 0) {
-                        zero_rows<kD, kWalk>(y1_smem(s), left, (left + 15) & ~15, lane);
-                        zero_rows<kD, kWalk>(y2_smem(s), left, (left + 15) & ~15, lane);
-                        fence_proxy_async_smem();
-                        __syncwarp();
+                    if (!wait(bar(kYFull, g) + round_bars, (int)ring_phase, 82)) break;
+                    if (--to_last == 0) {
+                        to_last = tiles_a_head;
+                        if (last_left < kWalk && (last_left & 15) != 0) {
+                            const uint32_t y1 = y1_smem(g) + (half != 0 ? (uint32_t)(kGroups * 2 * B::kWalkBytes) : 0u);
+                            zero_rows<kD, kWalk>(y1, last_left, (last_left + 15) & ~15, lane);
+                            zero_rows<kD, kWalk>(y1 + B::kWalkBytes, last_left, (last_left + 15) & ~15, lane);
+                            fence_proxy_async_smem();
+                            __syncwarp();
+                        }
                     }
                     tc_fence_after();
-                    scores(s);
+                    scores(g, y_round);
                 }
+                // the tile whose sums are due: kGroups - 1 before, in the stage after this one, of this round of the stages or the last
                 constexpr int kBehind = kGroups - 1;
-                if (it >= kBehind) {
-                    const int m = it - kBehind, ms = (s + kRing - kBehind) % kRing;            // the tile whose sums are due, and its stage
-                    if (!wait(bar(kPFull, ms % kGroups), ms / kGroups, 83)) break;             // a round of the ring has an even number of a group's tiles
+                const int m = it - kBehind, mg = (g + 1) % kGroups;
+                const bool same = g + 1 == kGroups;
+                if (m >= 0 && m < tiles) {
+                    if (!wait(bar(kPFull, mg), (int)(same ? half : half ^ 1u), 83)) break;
                     tc_fence_after();
-                    sums(ms, m == 0, (sums_left + 15) >> 4);
-                    sums_left -= kWalk;
-                    if (++sums_t == tiles_a_head) { sums_t = 0; sums_left = first_left; }
+                    int steps = kWalk / 16;
+                    if (--sums_to_last == 0) {
+                        sums_to_last = tiles_a_head;
+                        steps = last_steps;
+                    }
+                    sums(mg, same ? y_round : y_before, m == 0, steps);
+                    umma_commit_if(bar(kYEmpty, mg) + (same ? round_bars : before_bars), elected);
                     if (m == tiles - 1) umma_commit_if(bar(kDone, 0), elected);
                 }
-                left -= kWalk;
-                if (++t == tiles_a_head) { t = 0; left = first_left; }
             }
+            if (half != 0) ring_phase ^= 1u;
+            half ^= 1u;
         }
         __syncwarp();
     } else {
