@@ -74,7 +74,9 @@ packed_attention_kernel(const __grid_constant__ ForwardParams p)
     pdl_release_successors();
     const int head = blockIdx.x % p.heads;
     PackedTile tile;
-    if (!plan_tile<kTiles * 128>(p.plan, p.rows, p.sequences, blockIdx.x / p.heads, p.causal != 0, p.dev_status, tile)) return;
+    if ((int)(blockIdx.x / p.heads) >= plan_tiles<kTiles * 128>(p.plan, p.rows, p.sequences, p.dev_status)) return;
+    const int4 entry = plan_entry<kTiles * 128>(p.plan, p.rows, p.sequences, blockIdx.x / p.heads);
+    if (!plan_tile<kTiles * 128>(entry, p.rows, p.causal != 0, tile)) return;
 
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;

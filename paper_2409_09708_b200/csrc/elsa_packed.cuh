@@ -22,23 +22,36 @@ struct PackedTile {
     int begin, len, first;               // the sequence's rows [begin, begin + len); the tile starts at row `first` of the sequence
 };
 
-// Tile `index` of the plan's list of 128- or 256-row tiles; false where there is none, or where the plan is not one of these rows
-// and sequences (dev_status then tells).  last_first: tiles of a sequence in reverse order (the costly ones of a causal mask first).
-// index is below plan_capacity(), so the entry may be asked for beside the header.
+// How many tiles of 128 or 256 rows the plan lists; -1 where it is not one of these rows and sequences (dev_status then tells).
 template <int kTileRows>
-__device__ __forceinline__ bool plan_tile(const int* plan, int rows, int sequences, int index, bool last_first, uint32_t* dev_status, PackedTile& t)
+__device__ __forceinline__ int plan_tiles(const int* plan, int rows, int sequences, uint32_t* dev_status)
 {
-    const int4* list = reinterpret_cast<const int4*>(plan + kPlanHeader) + (kTileRows == 128 ? 0 : plan_capacity(rows, sequences, 128));
-    int4 head, e;
+    int4 head;
     int count;
     asm volatile("ld.global.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(head.x), "=r"(head.y), "=r"(head.z), "=r"(head.w) : "l"(plan));
     asm volatile("ld.global.s32 %0, [%1];" : "=r"(count) : "l"(plan + (kTileRows == 128 ? kPlanWord128 : kPlanWord256)));
-    asm volatile("ld.global.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(e.x), "=r"(e.y), "=r"(e.z), "=r"(e.w) : "l"(list + index));
     if (head.x != kPlanMagic || head.y != rows || head.z != sequences) {
         if (dev_status != nullptr && threadIdx.x == 0 && blockIdx.x == 0) atomicCAS(dev_status, 0u, (uint32_t)ELSA_ERR_SHAPE | (79u << 8));
-        return false;
+        return -1;
     }
-    if (index >= count) return false;
+    const int most = plan_capacity(rows, sequences, kTileRows);
+    return count < most ? count : most;
+}
+
+// The entry of a tile, for an index below plan_capacity(): the load alone, so that it may be made ahead.
+template <int kTileRows>
+__device__ __forceinline__ int4 plan_entry(const int* plan, int rows, int sequences, int index)
+{
+    const int4* list = reinterpret_cast<const int4*>(plan + kPlanHeader) + (kTileRows == 128 ? 0 : plan_capacity(rows, sequences, 128));
+    int4 e;
+    asm volatile("ld.global.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(e.x), "=r"(e.y), "=r"(e.z), "=r"(e.w) : "l"(list + index));
+    return e;
+}
+
+// last_first: tiles of a sequence in reverse order (the costly ones of a causal mask first).  False for an entry that is none.
+template <int kTileRows>
+__device__ __forceinline__ bool plan_tile(const int4& e, int rows, bool last_first, PackedTile& t)
+{
     t.begin = e.x;
     t.len = e.y;
     t.first = (last_first ? (e.y - 1) / kTileRows - e.z : e.z) * kTileRows;

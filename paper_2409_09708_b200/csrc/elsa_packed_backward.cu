@@ -27,18 +27,24 @@ namespace {
 
 constexpr int kWalk = 64;                // walked rows of a tile
 
-template <int kD>
+// kGroups: stages of S and T, each with four warps.  Heads of 128 columns have two of them on an SM.  Narrower heads have one in each of two
+// CTAs, where one's beginning and end run under the other's products, or three in one, which keep the tensor core busier once they
+// run: chosen by the sequences' mean length (12 heads of 64, us with one and with three: dq of 16 x 1024 rows 146 and 162, of 2 x 4736
+// with 8 heads 193 and 176; dk and dv of 64 images of 49 to 1024 rows 228 and 240, of 16 x 1024 164 and 150, of 2 x 4736 228 and 193).
+constexpr int kLongForQueries = 2048, kLongForKeys = 768;
+
+template <int kD, int kGroupsOf>
 struct BackwardShape {
-    static constexpr int kGroups = kD > 64 ? 2 : 3;                  // stages of S and T, each with four warps
-    static constexpr int kRing = 2 * kGroups;                        // tiles of walked rows on their way
+    static constexpr int kGroups = kGroupsOf;
+    static constexpr int kPerSm = kGroups == 1 ? 2 : 1;
+    static constexpr int kHalf = kGroups == 1 ? 2 : kGroups, kRing = 2 * kHalf;        // tiles of walked rows on their way
     static constexpr int kThreads = kGroups * 128 + 64;
-    static constexpr int kTmemCols = 512;
+    static constexpr int kTmemCols = 512 / kPerSm;
     static constexpr int kKeptBytes = TileShape<kD>::bytes(128), kWalkBytes = TileShape<kD>::bytes(kWalk);
     static constexpr int kAcc1 = 128 * kGroups, kAcc2 = kAcc1 + kD;  // tensor-memory columns; stage g: S at 128 g, T at 128 g + 64
     static_assert(kAcc2 + kD <= kTmemCols, "tensor memory");
     static constexpr int kVectorBytes = 2 * kWalk * 4;               // -lse log2(e), -delta
-    static constexpr int kSmemBytes = 2 * kKeptBytes + kRing * (2 * kWalkBytes + kVectorBytes) + 1024 /* delta of the kept rows */ +
-                                      1024 /* alignment */ + 256 /* barriers */;
+    static constexpr int kSmemBytes = 2 * kKeptBytes + kRing * (2 * kWalkBytes + kVectorBytes) + 1024 /* alignment */ + 256 /* barriers */;
 };
 
 struct BackwardParams {
@@ -71,17 +77,19 @@ __device__ __forceinline__ void copies_arrive(uint32_t bar)
     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
 
-template <bool kBf16, int kD, bool kKeys>
-__global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attention_backward_kernel(const __grid_constant__ BackwardParams p)
+template <bool kBf16, int kD, bool kKeys, int kGroupsOf>
+__global__ void __launch_bounds__(BackwardShape<kD, kGroupsOf>::kThreads, BackwardShape<kD, kGroupsOf>::kPerSm) packed_attention_backward_kernel(const __grid_constant__ BackwardParams p)
 {
-    using B = BackwardShape<kD>;
+    using B = BackwardShape<kD, kGroupsOf>;
     pdl_wait_for_predecessors();
     pdl_release_successors();
     const int kept_heads = kKeys ? p.kv_heads : p.heads;
     const int head = blockIdx.x % kept_heads;
     PackedTile tile;
     // under a causal mask the last query tiles and the first key tiles have the most to do
-    if (!plan_tile<128>(p.plan, p.rows, p.sequences, blockIdx.x / kept_heads, p.causal != 0 && !kKeys, p.dev_status, tile)) return;
+    if ((int)(blockIdx.x / kept_heads) >= plan_tiles<128>(p.plan, p.rows, p.sequences, p.dev_status)) return;
+    const int4 entry = plan_entry<128>(p.plan, p.rows, p.sequences, blockIdx.x / kept_heads);
+    if (!plan_tile<128>(entry, p.rows, p.causal != 0 && !kKeys, tile)) return;
 
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -89,8 +97,7 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
     auto y1_smem = [&](int s) { return smem_base + (uint32_t)(2 * B::kKeptBytes + 2 * s * B::kWalkBytes); };
     auto y2_smem = [&](int s) { return y1_smem(s) + (uint32_t)B::kWalkBytes; };
     const uint32_t vectors = smem_base + (uint32_t)(2 * B::kKeptBytes + 2 * B::kRing * B::kWalkBytes);
-    const uint32_t kept_delta = vectors + B::kRing * B::kVectorBytes;                     // [2][128] floats
-    const uint32_t bars = kept_delta + 1024;
+    const uint32_t bars = vectors + B::kRing * B::kVectorBytes;
     enum { kXFull = 0, kYFull = 1, kYEmpty = kYFull + B::kRing, kSFull = kYEmpty + B::kRing, kPFull = kSFull + B::kGroups, kDone = kPFull + B::kGroups, kBars };
     auto bar = [&](int which, int i) { return bars + (uint32_t)(8 * (which + i)); };
     const uint32_t tmem_holder_addr = bars + 8 * kBars;
@@ -176,12 +183,14 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
         const uint32_t x1_desc = Desc::k_major(uniform(smem_base)), x2_desc = x1_desc + (uint32_t)(B::kKeptBytes >> 4);
         const uint32_t y1_rows = Desc::k_major(uniform(y1_smem(0))), y1_cols = Desc::template mn_major<kWalk>(uniform(y1_smem(0)));
         constexpr uint32_t kY2 = (uint32_t)(B::kWalkBytes >> 4);
-        // The loop is unrolled over the stages, so that their addresses are constants, and does little else than wait and issue: while this warp
-        // works something out the tensor core idles.  S and T of a tile are issued kGroups - 1 tiles ahead of the sums.  The ring has two
-        // rounds of the stages: y_round is the offset of the one that S and T (the sums) are in, as descriptors count.
-        constexpr uint32_t kRound = (uint32_t)(kGroups * 2) * kY2;
-        auto scores = [&](int g, uint32_t y_round) {
-            const uint32_t t_s = tmem_u + (uint32_t)(128 * g), y_at = y1_rows + y_round + (uint32_t)(g * 2) * kY2;
+        // The loop is unrolled over half the ring, so that addresses are constants, and does little else than wait and issue: while this warp
+        // works something out, or fetches code, the tensor core idles.  S and T of a tile are issued kGroups - 1 tiles ahead of the sums.
+        // y_round is the offset of the half that S and T are in, as descriptors count.
+        constexpr int kHalf = B::kHalf, kBehind = kGroups - 1;
+        constexpr uint32_t kRound = (uint32_t)(kHalf * 2) * kY2;
+        auto scores = [&](int u, uint32_t y_round) {
+            const int g = u % kGroups;
+            const uint32_t t_s = tmem_u + (uint32_t)(128 * g), y_at = y1_rows + y_round + (uint32_t)(u * 2) * kY2;
 #pragma unroll
             for (int k = 0; k < kD / 16; ++k)
                 umma_f16_if(t_s, Desc::of(x1_desc + Desc::k_step(128, k)), Desc::of(y_at + Desc::k_step(kWalk, k)), p.idesc_s, (uint32_t)(k != 0), elected);
@@ -190,8 +199,8 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
                 umma_f16_if(t_s + 64, Desc::of(x2_desc + Desc::k_step(128, k)), Desc::of(y_at + kY2 + Desc::k_step(kWalk, k)), p.idesc_s, (uint32_t)(k != 0), elected);
             umma_commit_if(bar(kSFull, g), elected);
         };
-        auto sums = [&](int g, uint32_t y_round, bool first, int steps) {
-            const uint32_t t_s = tmem_u + (uint32_t)(128 * g), y_at = y1_cols + y_round + (uint32_t)(g * 2) * kY2;
+        auto sums = [&](int u, uint32_t y_round, bool first, int steps) {
+            const uint32_t t_s = tmem_u + (uint32_t)(128 * (u % kGroups)), y_at = y1_cols + y_round + (uint32_t)(u * 2) * kY2;
             auto p_step = [&](int k) {
                 umma_f16_ts_if(tmem_u + B::kAcc1, t_s + (uint32_t)(8 * k), Desc::of(y_at + kY2 + (uint32_t)k * Desc::kRowsStep), p.idesc_acc,
                                k != 0 ? 1u : first ? 0u : 1u, elected);
@@ -220,19 +229,19 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
         const int last_steps = last_left >= kWalk ? kWalk / 16 : (last_left + 15) / 16;
         int to_last = tiles_a_head, sums_to_last = tiles_a_head;
         wait(bar(kXFull, 0), 0, 81);
-        uint32_t half = 0, ring_phase = 0;                           // round of the stages, phase of the ring's barriers
-        for (int it0 = 0; ok && it0 < tiles + kGroups - 1; it0 += kGroups) {
+        uint32_t half = 0, ring_phase = 0;                           // half of the ring, phase of its barriers
+        for (int it0 = 0; ok && it0 < tiles + kBehind; it0 += kHalf) {
             const uint32_t y_round = half != 0 ? kRound : 0u, y_before = kRound - y_round;
-            const uint32_t round_bars = half != 0 ? 8u * kGroups : 0u, before_bars = 8u * kGroups - round_bars;
+            const uint32_t round_bars = half != 0 ? 8u * kHalf : 0u, before_bars = 8u * kHalf - round_bars;
 #pragma unroll
-            for (int g = 0; g < kGroups; ++g) {
-                const int it = it0 + g;
+            for (int u = 0; u < kHalf; ++u) {
+                const int it = it0 + u;
                 if (it < tiles) {
-                    if (!wait(bar(kYFull, g) + round_bars, (int)ring_phase, 82)) break;
+                    if (!wait(bar(kYFull, u) + round_bars, (int)ring_phase, 82)) break;
                     if (--to_last == 0) {
                         to_last = tiles_a_head;
                         if (last_left < kWalk && (last_left & 15) != 0) {
-                            const uint32_t y1 = y1_smem(g) + (half != 0 ? (uint32_t)(kGroups * 2 * B::kWalkBytes) : 0u);
+                            const uint32_t y1 = y1_smem(u) + (half != 0 ? (uint32_t)(kHalf * 2 * B::kWalkBytes) : 0u);
                             zero_rows<kD, kWalk>(y1, last_left, (last_left + 15) & ~15, lane);
                             zero_rows<kD, kWalk>(y1 + B::kWalkBytes, last_left, (last_left + 15) & ~15, lane);
                             fence_proxy_async_smem();
@@ -240,22 +249,21 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
                         }
                     }
                     tc_fence_after();
-                    scores(g, y_round);
+                    scores(u, y_round);
                 }
-                // the tile whose sums are due: kGroups - 1 before, in the stage after this one, of this round of the stages or the last
-                constexpr int kBehind = kGroups - 1;
-                const int m = it - kBehind, mg = (g + 1) % kGroups;
-                const bool same = g + 1 == kGroups;
+                // the tile whose sums are due: kBehind tiles back, in this half of the ring or the other
+                const int m = it - kBehind, mu = (u + kHalf - kBehind) % kHalf;
+                const bool same = u >= kBehind;
                 if (m >= 0 && m < tiles) {
-                    if (!wait(bar(kPFull, mg), (int)(same ? half : half ^ 1u), 83)) break;
+                    if (!wait(bar(kPFull, mu % kGroups), kGroups == 1 ? u & 1 : (int)(same ? half : half ^ 1u), 83)) break;
                     tc_fence_after();
                     int steps = kWalk / 16;
                     if (--sums_to_last == 0) {
                         sums_to_last = tiles_a_head;
                         steps = last_steps;
                     }
-                    sums(mg, same ? y_round : y_before, m == 0, steps);
-                    umma_commit_if(bar(kYEmpty, mg) + (same ? round_bars : before_bars), elected);
+                    sums(mu, same ? y_round : y_before, m == 0, steps);
+                    umma_commit_if(bar(kYEmpty, mu) + (same ? round_bars : before_bars), elected);
                     if (m == tiles - 1) umma_commit_if(bar(kDone, 0), elected);
                 }
             }
@@ -271,16 +279,15 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
         const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16);
         float minus_lse = 0.f, minus_delta = 0.f;
         if constexpr (!kKeys) {
-            // delta: half a row by each of two groups
-            const size_t at = (size_t)head * (size_t)p.rows + (size_t)(tile.begin + row);
-            constexpr int kPart = kD / 2;
-            float part = 0.f;
-            if (exists) minus_lse = -1.4426950408889634f * __ldg(p.lse + at);
-            if (exists && g < 2) {
-                const uint4* a4 = reinterpret_cast<const uint4*>(p.a + (long long)(tile.begin + row) * p.a_pitch + head * kD + g * kPart);
-                const uint4* d4 = reinterpret_cast<const uint4*>(p.da + (long long)(tile.begin + row) * p.da_pitch + head * kD + g * kPart);
+            // delta, by each group for itself: an exchange would be one more wait, and the rows are in the first-level cache
+            if (exists) {
+                const size_t at = (size_t)head * (size_t)p.rows + (size_t)(tile.begin + row);
+                const uint4* a4 = reinterpret_cast<const uint4*>(p.a + (long long)(tile.begin + row) * p.a_pitch + head * kD);
+                const uint4* d4 = reinterpret_cast<const uint4*>(p.da + (long long)(tile.begin + row) * p.da_pitch + head * kD);
+                const float lse = __ldg(p.lse + at);
+                float part = 0.f;
 #pragma unroll
-                for (int v = 0; v < kPart / 8; ++v) {
+                for (int v = 0; v < kD / 8; ++v) {
                     const uint4 x = __ldg(a4 + v), y = __ldg(d4 + v);
                     const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
@@ -289,20 +296,12 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
                         part = fmaf(u.x, w.x, fmaf(u.y, w.y, part));
                     }
                 }
-            }
-            {
-                const uint32_t mine = kept_delta + (uint32_t)(4 * (quarter * 32 + lane));
-                if (g < 2) asm volatile("st.shared.f32 [%0], %1;" ::"r"(mine + (uint32_t)(512 * g)), "f"(part) : "memory");
-                asm volatile("bar.sync 1, %0;" ::"n"(128 * kGroups) : "memory");
-                float first, second;
-                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(first) : "r"(mine) : "memory");
-                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(second) : "r"(mine + 512u) : "memory");
-                part = first + second;
-            }
-            minus_delta = -part;
-            if (g == 0 && exists) {
-                p.minus_lse[at] = minus_lse;
-                if (n > 1) p.minus_delta[at] = minus_delta;
+                minus_lse = -1.4426950408889634f * lse;
+                minus_delta = -part;
+                if (g == 0) {
+                    p.minus_lse[at] = minus_lse;
+                    if (n > 1) p.minus_delta[at] = minus_delta;
+                }
             }
         }
         const uint64_t scale2 = f32x2(p.scale_log2, p.scale_log2);
@@ -389,13 +388,13 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
         if (ok && row0 < tile.len && wait(bar(kDone, 0), 0, 86)) {
             tc_fence_after();
             // all copies and products have ended: the ring is staging room
-            const uint32_t stage = y1_smem(0) + (uint32_t)(4096 * warp);
+            const uint32_t stage = y1_smem(0) + (uint32_t)(32 * 2 * TileShape<kD>::kCols * warp);
             const long long first = tile.begin + row0;
             if constexpr (kKeys) {
                 constexpr int kCols = TileShape<kD>::kCols;
 #pragma unroll
-                for (int o = 0; o < 2; ++o) {                        // dv by one group, dk by another
-                    if (o != g) continue;
+                for (int o = 0; o < 2; ++o) {                        // dv, then dk; one by each of the first two groups where there are more than one
+                    if (kGroups > 1 && o != g) continue;
                     uint16_t* dst = (o == 0 ? p.out1 + first * p.out1_pitch : p.out2 + first * p.out2_pitch) + head * kD;
 #pragma unroll
                     for (int c = 0; c < kD; c += kCols)
@@ -403,8 +402,8 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
                                                  o == 0 ? p.out1_pitch : p.out2_pitch, tile.len - row0, lane);
                 }
             } else {
-                // half the columns by each of two groups; heads of 32 columns by the first alone
-                constexpr int kCols = kD / 2 < 32 ? 32 : kD / 2;
+                // the columns, in halves by the first two groups where there are more than one and each half has 32
+                constexpr int kCols = kGroups > 1 && kD > 32 ? kD / 2 : kD;
                 if (kCols * g < kD)
                     store_rows<kBf16, kCols>(t_lane + (uint32_t)(B::kAcc2 + kCols * g), p.scale, stage, p.out2 + first * p.out2_pitch + head * kD + kCols * g,
                                              p.out2_pitch, tile.len - row0, lane);
@@ -420,12 +419,12 @@ __global__ void __launch_bounds__(BackwardShape<kD>::kThreads, 1) packed_attenti
     }
 }
 
-template <bool kBf16, int kD, bool kKeys>
+template <bool kBf16, int kD, bool kKeys, int kGroupsOf>
 elsa_status launch(const BackwardParams& p, cudaStream_t stream, const DeviceInfo& dev)
 {
-    using B = BackwardShape<kD>;
-    static_assert(2 * B::kRing * B::kWalkBytes >= 4 * B::kGroups * 4096, "staging room");
-    auto kernel = packed_attention_backward_kernel<kBf16, kD, kKeys>;
+    using B = BackwardShape<kD, kGroupsOf>;
+    static_assert(2 * B::kRing * B::kWalkBytes >= 4 * B::kGroups * 32 * 2 * TileShape<kD>::kCols, "staging room");
+    auto kernel = packed_attention_backward_kernel<kBf16, kD, kKeys, kGroupsOf>;
     static std::atomic<bool> attr_set[64];
     const int slot = dev.device & 63;
     if (!attr_set[slot].load(std::memory_order_acquire)) {
@@ -446,8 +445,16 @@ elsa_status launch(const BackwardParams& p, cudaStream_t stream, const DeviceInf
 template <bool kBf16, int kD>
 elsa_status launch_both(const BackwardParams& queries, const BackwardParams& keys, cudaStream_t stream, const DeviceInfo& dev)
 {
-    const elsa_status st = launch<kBf16, kD, false>(queries, stream, dev);
-    return st != ELSA_OK ? st : launch<kBf16, kD, true>(keys, stream, dev);
+    elsa_status st;
+    if constexpr (kD > 64) {
+        st = launch<kBf16, kD, false, 2>(queries, stream, dev);
+        return st != ELSA_OK ? st : launch<kBf16, kD, true, 2>(keys, stream, dev);
+    } else {
+        const int mean = queries.rows / queries.sequences;
+        st = mean >= kLongForQueries ? launch<kBf16, kD, false, 3>(queries, stream, dev) : launch<kBf16, kD, false, 1>(queries, stream, dev);
+        if (st != ELSA_OK) return st;
+        return mean >= kLongForKeys ? launch<kBf16, kD, true, 3>(keys, stream, dev) : launch<kBf16, kD, true, 1>(keys, stream, dev);
+    }
 }
 
 }  // namespace

@@ -138,9 +138,12 @@ def test_many_items(lib, D, dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("causal", [False, True], ids=["full", "causal"])
-@pytest.mark.parametrize("D", [64, 128])
-def test_long_sequence(lib, D, causal):
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_long_sequences(lib, D, causal):
+    """Of a length that has the gradient's kernels of long sequences, beside short ones that they then meet too."""
     check(lib, [4500], 2, 1, D, causal, torch.bfloat16)
+    check(lib, [2600, 1, 4000], 2, 2, D, causal, torch.float16)
+    check(lib, [1500, 70, 999], 2, 1, D, causal, torch.bfloat16)
 
 
 @pytest.mark.gpu
@@ -209,15 +212,15 @@ def test_other_rows_take_no_part_and_stay(lib, causal, D, filler):
 @pytest.mark.parametrize("D", [32, 64, 128])
 def test_tiles_with_idle_warps_many_times(lib, D):
     """Last tiles of which some warps have no rows, beside full ones on the same SM: the same bits in each of many runs."""
-    lengths = np.random.default_rng(3).integers(1, 700, 60).tolist()
-    qkv, (q, k, v), da = inputs(lengths, 3, 3, D, torch.bfloat16)
-    plan = lib.make_packed_plan(offsets_of(lengths))
-    first = None
-    for _ in range(100):
-        a, lse = lib.elsa_packed_attention(q, k, v, plan, 3, want_lse=True)
-        got = (a, lse) + lib.elsa_packed_attention_backward(da, q, k, v, a, lse, plan, 3)
-        first = first or got
-        assert all(torch.equal(x, y) for x, y in zip(first, got))
+    for lengths in (np.random.default_rng(3).integers(1, 700, 60).tolist(), [3000, 2500, 130, 3100, 5000]):
+        qkv, (q, k, v), da = inputs(lengths, 3, 3, D, torch.bfloat16)
+        plan = lib.make_packed_plan(offsets_of(lengths))
+        first = None
+        for _ in range(100):
+            a, lse = lib.elsa_packed_attention(q, k, v, plan, 3, want_lse=True)
+            got = (a, lse) + lib.elsa_packed_attention_backward(da, q, k, v, a, lse, plan, 3)
+            first = first or got
+            assert all(torch.equal(x, y) for x, y in zip(first, got))
 
 
 @pytest.mark.gpu
