@@ -526,7 +526,7 @@ elsa_status elsa_nm_linear_backward(const void* dY, const void* X, int rows, con
  * video or causal sequences: LayerNorm with its gradient, rotary positions, attention over packed sequences with its
  * gradient.  16-bit tensors of one dtype, fp32 arithmetic, one rounding of each stored value; no atomics on results: the
  * same inputs give the same bits every time.  DEVICE pointers, 16-byte aligned, unless stated otherwise; asynchronous on
- * `stream`; errors as for elsa_nm_linear.
+ * `stream`; errors as for elsa_nm_linear.  At most 2^30 rows.  Calls that share a workspace must be stream-ordered.
  *
  * LayerNorm of rows of dim values (a multiple of 8):
  *     s = x + residual (rounded to dtype; without a residual s is x)
@@ -583,7 +583,8 @@ elsa_status elsa_rotary(const void* x, long long x_pitch, const int32_t* positio
  * one in v, or in da, may reach every row of it, a causal mask or not.
  *
  * elsa_packed_plan cuts the sequences into tiles once for any number of calls with the same offsets (all layers, both
- * directions): plan is elsa_packed_plan_bytes(...) of device memory that the calls read.  Offsets that break the rules
+ * directions): plan is elsa_packed_plan_bytes(...) of device memory that the calls read, on any stream ordered behind it; it stays
+ * until the last of them (a captured one's last replay) has run, the offsets only until elsa_packed_plan has.  Offsets that break the rules
  * make an empty plan, and dev_status (if given) receives ELSA_ERR_SHAPE | 69 << 8; a plan made for other rows or another
  * number of sequences makes a call that computes nothing, ELSA_ERR_SHAPE | 79 << 8.
  * q [rows][heads * head_dim], k and v [rows][kv_heads * head_dim]: heads side by side in a row, rows *_pitch values apart

@@ -532,7 +532,8 @@ class PackedPlan:
 
 def make_packed_plan(offsets, rows=None, device="cuda", dev_status=None, stream=None):
     """Plan of a batch with sequence i in rows [offsets[i], offsets[i + 1]).  offsets: a list or a CPU tensor, checked here, or an
-    int32 tensor on the device, checked there (dev_status); rows: of the tensors, at least the last offset (default: it)."""
+    int32 tensor on the device, checked there (dev_status); rows: of the tensors, at least the last offset (default: it).  A
+    captured call reads the plan at every replay: keep it."""
     full = False
     if not torch.is_tensor(offsets) or not offsets.is_cuda:
         host = [int(o) for o in (offsets.tolist() if torch.is_tensor(offsets) else offsets)]

@@ -1718,13 +1718,25 @@ int elsa_profile_stop(elsa_kernel_time* records, int capacity)
 
 unsigned long long elsa_launch_count(void) { return g_launches.load(std::memory_order_relaxed); }
 
+namespace {
+// Rows of the calls below: the kernels step through them in ints.
+constexpr int kMostRows = 1 << 30;
+elsa_status check_rows(int rows)
+{
+    if (rows <= 0) return fail(ELSA_ERR_SHAPE, "non-positive rows=%d", rows);
+    return rows <= kMostRows ? ELSA_OK : fail(ELSA_ERR_SHAPE, "rows=%d is above 2^30", rows);
+}
+}  // namespace
+
 elsa_status elsa_layer_norm(const void* x, const void* residual, const void* gain, const void* bias, int rows, int dim, float eps,
                             elsa_dtype dtype, void* s, void* y, float* stats, void* stream)
 {
     if (!x || !gain || !bias || !y) return fail(ELSA_ERR_NULL, "x, gain, bias and y must not be NULL");
     if ((residual == nullptr) != (s == nullptr)) return fail(ELSA_ERR_NULL, "residual and s go together");
     if (dtype != ELSA_F16 && dtype != ELSA_BF16) return fail(ELSA_ERR_DTYPE, "dtype %d is neither ELSA_F16 nor ELSA_BF16", (int)dtype);
-    if (rows <= 0 || dim <= 0) return fail(ELSA_ERR_SHAPE, "non-positive dimension (rows=%d, dim=%d)", rows, dim);
+    elsa_status st = check_rows(rows);
+    if (st != ELSA_OK) return st;
+    if (dim <= 0) return fail(ELSA_ERR_SHAPE, "non-positive dim=%d", dim);
     if (!(eps >= 0.f)) return fail(ELSA_ERR_SHAPE, "eps=%g must not be negative", (double)eps);
     if (dim % 8 != 0) return fail(ELSA_ERR_ALIGN, "dim=%d must be a multiple of 8 (16-byte row pitch)", dim);
     if (!aligned16(x) || !aligned16(residual) || !aligned16(gain) || !aligned16(bias) || !aligned16(s) || !aligned16(y) || ((uintptr_t)stats & 7u))
@@ -1737,7 +1749,7 @@ elsa_status elsa_layer_norm(const void* x, const void* residual, const void* gai
 
 size_t elsa_layer_norm_backward_workspace_bytes(int rows, int dim)
 {
-    return rows <= 0 || dim <= 0 || dim % 8 != 0 || !layer_norm_columns_suits(dim) ? 0 : layer_norm_backward_workspace(rows, dim);
+    return rows <= 0 || rows > kMostRows || dim <= 0 || dim % 8 != 0 || !layer_norm_columns_suits(dim) ? 0 : layer_norm_backward_workspace(rows, dim);
 }
 
 elsa_status elsa_layer_norm_backward(const void* dy, const void* s, const float* stats, const void* gain, const void* ds, int rows, int dim,
@@ -1746,7 +1758,9 @@ elsa_status elsa_layer_norm_backward(const void* dy, const void* s, const float*
     if (!dy || !s || !stats || !gain) return fail(ELSA_ERR_NULL, "dy, s, stats and gain must not be NULL");
     if (!dx && !dgain && !dbias) return fail(ELSA_ERR_NULL, "one of dx, dgain and dbias must be given");
     if (dtype != ELSA_F16 && dtype != ELSA_BF16) return fail(ELSA_ERR_DTYPE, "dtype %d is neither ELSA_F16 nor ELSA_BF16", (int)dtype);
-    if (rows <= 0 || dim <= 0) return fail(ELSA_ERR_SHAPE, "non-positive dimension (rows=%d, dim=%d)", rows, dim);
+    elsa_status st = check_rows(rows);
+    if (st != ELSA_OK) return st;
+    if (dim <= 0) return fail(ELSA_ERR_SHAPE, "non-positive dim=%d", dim);
     if (dim % 8 != 0) return fail(ELSA_ERR_ALIGN, "dim=%d must be a multiple of 8 (16-byte row pitch)", dim);
     if (!layer_norm_columns_suits(dim)) return fail(ELSA_ERR_SHAPE, "dim=%d is above 16384", dim);
     if (!aligned16(dy) || !aligned16(s) || !aligned16(gain) || !aligned16(ds) || !aligned16(dx) || !aligned16(dgain) || !aligned16(dbias) ||
@@ -1770,7 +1784,9 @@ elsa_status elsa_rotary(const void* x, long long x_pitch, const int32_t* positio
     if (plan->head_dim < 16 || plan->head_dim > 2 * ELSA_ROTARY_MAX_PAIRS || plan->head_dim % 16 != 0 || plan->axes < 1 ||
         plan->axes > ELSA_ROTARY_MAX_AXES)
         return fail(ELSA_ERR_SHAPE, "the plan is none that elsa_rotary_make_plan makes (head_dim=%d, axes=%d)", plan->head_dim, plan->axes);
-    if (rows <= 0 || heads <= 0) return fail(ELSA_ERR_SHAPE, "non-positive dimension (rows=%d, heads=%d)", rows, heads);
+    elsa_status st = check_rows(rows);
+    if (st != ELSA_OK) return st;
+    if (heads <= 0) return fail(ELSA_ERR_SHAPE, "non-positive heads=%d", heads);
     const long long width = (long long)heads * plan->head_dim;
     if (x_pitch < width || y_pitch < width)
         return fail(ELSA_ERR_SHAPE, "x_pitch=%lld and y_pitch=%lld must be at least %d heads * %d", x_pitch, y_pitch, heads, plan->head_dim);
@@ -1781,12 +1797,14 @@ elsa_status elsa_rotary(const void* x, long long x_pitch, const int32_t* positio
     return launch_rotary((const uint16_t*)x, x_pitch, positions, *plan, rows, heads, inverse != 0, dtype, (uint16_t*)y, y_pitch, (cudaStream_t)stream);
 }
 
-size_t elsa_packed_plan_bytes(int rows, int sequences) { return rows <= 0 || sequences <= 0 ? 0 : packed_plan_bytes(rows, sequences); }
+size_t elsa_packed_plan_bytes(int rows, int sequences) { return rows <= 0 || rows > kMostRows || sequences <= 0 ? 0 : packed_plan_bytes(rows, sequences); }
 
 elsa_status elsa_packed_plan(const int32_t* offsets, int sequences, int rows, void* plan, size_t plan_bytes, uint32_t* dev_status, void* stream)
 {
     if (!offsets || !plan) return fail(ELSA_ERR_NULL, "offsets and plan must not be NULL");
-    if (sequences <= 0 || rows <= 0) return fail(ELSA_ERR_SHAPE, "non-positive dimension (sequences=%d, rows=%d)", sequences, rows);
+    elsa_status st = check_rows(rows);
+    if (st != ELSA_OK) return st;
+    if (sequences <= 0) return fail(ELSA_ERR_SHAPE, "non-positive sequences=%d", sequences);
     if (((uintptr_t)offsets & 3u) || !aligned16(plan)) return fail(ELSA_ERR_ALIGN, "offsets must be 4-byte aligned, plan 16-byte aligned");
     const size_t need = packed_plan_bytes(rows, sequences);
     if (plan_bytes < need) return fail(ELSA_ERR_WORKSPACE, "plan of %zu bytes needed, %zu given", need, plan_bytes);
@@ -1805,15 +1823,17 @@ elsa_status check_packed(const elsa_packed_qkv* in, int dtype, const void* plan,
 {
     if (!in || !plan) return fail(ELSA_ERR_NULL, "in and plan must not be NULL");
     if (dtype != ELSA_F16 && dtype != ELSA_BF16) return fail(ELSA_ERR_DTYPE, "dtype %d is neither ELSA_F16 nor ELSA_BF16", dtype);
-    if (in->rows <= 0 || in->heads <= 0 || in->kv_heads <= 0 || sequences <= 0)
-        return fail(ELSA_ERR_SHAPE, "non-positive dimension (rows=%d, heads=%d, kv_heads=%d, sequences=%d)", in->rows, in->heads, in->kv_heads, sequences);
+    elsa_status st = check_rows(in->rows);
+    if (st != ELSA_OK) return st;
+    if (in->heads <= 0 || in->kv_heads <= 0 || sequences <= 0)
+        return fail(ELSA_ERR_SHAPE, "non-positive dimension (heads=%d, kv_heads=%d, sequences=%d)", in->heads, in->kv_heads, sequences);
     if (in->head_dim != 32 && in->head_dim != 64 && in->head_dim != 128) return fail(ELSA_ERR_SHAPE, "head_dim=%d is neither 32, 64 nor 128", in->head_dim);
     if (in->heads % in->kv_heads != 0) return fail(ELSA_ERR_SHAPE, "heads=%d is not a multiple of kv_heads=%d", in->heads, in->kv_heads);
     if ((long long)in->heads * in->head_dim > 0x7fffffffLL) return fail(ELSA_ERR_SHAPE, "heads * head_dim does not fit an int");
     if (!(in->scale - in->scale == 0.f)) return fail(ELSA_ERR_SHAPE, "scale is not finite");
     if (!aligned16(plan)) return fail(ELSA_ERR_ALIGN, "plan must be 16-byte aligned");
     const long long wide = (long long)in->heads * in->head_dim, narrow = (long long)in->kv_heads * in->head_dim;
-    elsa_status st = check_heads("q", in->q, in->q_pitch, wide);
+    st = check_heads("q", in->q, in->q_pitch, wide);
     if (st == ELSA_OK) st = check_heads("k", in->k, in->k_pitch, narrow);
     if (st == ELSA_OK) st = check_heads("v", in->v, in->v_pitch, narrow);
     return st;
@@ -1830,7 +1850,7 @@ elsa_status elsa_packed_attention(const elsa_packed_qkv* in, elsa_dtype dtype, c
     return launch_packed_attention(*in, dtype, (const int*)plan, sequences, (uint16_t*)a, a_pitch, lse, dev_status, (cudaStream_t)stream);
 }
 
-size_t elsa_packed_attention_workspace_bytes(int rows, int heads) { return rows <= 0 || heads <= 0 ? 0 : packed_attention_workspace(rows, heads); }
+size_t elsa_packed_attention_workspace_bytes(int rows, int heads) { return rows <= 0 || rows > kMostRows || heads <= 0 ? 0 : packed_attention_workspace(rows, heads); }
 
 elsa_status elsa_packed_attention_backward(const elsa_packed_qkv* in, elsa_dtype dtype, const void* plan, int sequences, const void* a,
                                            long long a_pitch, const float* lse, const void* da, long long da_pitch, void* dq, long long dq_pitch,

@@ -31,7 +31,7 @@ def test_layer_norm(lib):
                                                stream=None))
     for n in ("x", "gain", "bias", "y", "s", "residual"):
         assert call(**{n: None}) == NULL, n
-    for kw in (dict(rows=0), dict(rows=-1), dict(dim=0), dict(eps=-1.0), dict(eps=float("nan"))):
+    for kw in (dict(rows=0), dict(rows=-1), dict(rows=(1 << 30) + 1), dict(dim=0), dict(eps=-1.0), dict(eps=float("nan"))):
         assert call(**kw) == SHAPE, kw
     assert call(dt=2) == DTYPE
     for kw in (dict(dim=60), dict(x=FAKE + 2), dict(y=FAKE + 8), dict(gain=FAKE + 4), dict(bias=FAKE + 2), dict(s=FAKE + 2), dict(residual=FAKE + 2),
@@ -46,7 +46,7 @@ def test_layer_norm_backward(lib):
     for n in ("dy", "s", "stats", "gain"):
         assert call(**{n: None}) == NULL, n
     assert call(dx=None, dgain=None, dbias=None) == NULL
-    for kw in (dict(rows=0), dict(dim=-8), dict(dim=16392)):
+    for kw in (dict(rows=0), dict(rows=(1 << 30) + 1), dict(dim=-8), dict(dim=16392)):
         assert call(**kw) == SHAPE, kw
     assert call(dt=-1) == DTYPE
     for kw in (dict(dim=20), dict(dy=FAKE + 2), dict(s=FAKE + 2), dict(ds=FAKE + 2), dict(dx=FAKE + 2), dict(dgain=FAKE + 2), dict(dbias=FAKE + 2),
@@ -65,7 +65,7 @@ def test_rotary(lib):
     call = caller(lib._rotary, names, dict(x=FAKE, xp=256, positions=FAKE, plan=ctypes.byref(plan), rows=3, heads=4, inverse=0, dt=0, y=WORK, yp=256, stream=None))
     for n in ("x", "positions", "plan", "y"):
         assert call(**{n: None}) == NULL, n
-    for kw in (dict(rows=0), dict(heads=0), dict(xp=248), dict(yp=248), dict(heads=5), dict(y=FAKE, yp=264), dict(plan=ctypes.byref(lib.ElsaRotaryPlan()))):
+    for kw in (dict(rows=0), dict(rows=(1 << 30) + 1), dict(heads=0), dict(xp=248), dict(yp=248), dict(heads=5), dict(y=FAKE, yp=264), dict(plan=ctypes.byref(lib.ElsaRotaryPlan()))):
         assert call(**kw) == SHAPE, kw
     for field, value in (("head_dim", 72), ("head_dim", 512), ("axes", 0), ("axes", 5)):
         other = lib.make_rotary_plan(64, [16, 16])
@@ -80,7 +80,7 @@ def test_packed_plan(lib):
     names = "offsets sequences rows plan bytes status stream".split()
     call = caller(lib._packed_plan, names, dict(offsets=FAKE, sequences=3, rows=500, plan=WORK, bytes=1 << 20, status=None, stream=None))
     assert call(offsets=None) == NULL and call(plan=None) == NULL
-    assert call(sequences=0) == SHAPE and call(rows=0) == SHAPE
+    assert call(sequences=0) == SHAPE and call(rows=0) == SHAPE and call(rows=(1 << 30) + 1) == SHAPE
     assert call(offsets=FAKE + 2) == ALIGN and call(plan=WORK + 8) == ALIGN
     need = int(lib._packed_plan_bytes(500, 3))
     assert need == 64 + 16 * ((500 // 128 + 3) + (500 // 256 + 3)) and call(bytes=need - 1) == WORKSPACE
@@ -99,7 +99,7 @@ def qkv_of(lib, **kw):
     return ctypes.byref(lib.ElsaPackedQkv(*[a[n] for n, _ in lib.ElsaPackedQkv._fields_]))
 
 
-COMMON = [(dict(q=None), NULL), (dict(k=None), NULL), (dict(v=None), NULL), (dict(rows=0), SHAPE), (dict(heads=0), SHAPE), (dict(kv_heads=0), SHAPE),
+COMMON = [(dict(q=None), NULL), (dict(k=None), NULL), (dict(v=None), NULL), (dict(rows=0), SHAPE), (dict(rows=(1 << 30) + 1), SHAPE), (dict(heads=0), SHAPE), (dict(kv_heads=0), SHAPE),
           (dict(kv_heads=3), SHAPE), (dict(head_dim=48), SHAPE), (dict(head_dim=0), SHAPE), (dict(head_dim=256), SHAPE), (dict(scale=float("inf")), SHAPE),
           (dict(scale=float("nan")), SHAPE), (dict(q_pitch=248), SHAPE), (dict(k_pitch=120), SHAPE), (dict(v_pitch=0), SHAPE), (dict(q_pitch=260), ALIGN),
           (dict(k_pitch=132), ALIGN), (dict(q=FAKE + 8), ALIGN), (dict(v=FAKE + 2), ALIGN), (dict(heads=1 << 28, kv_heads=1, q_pitch=1 << 40), SHAPE)]

@@ -254,6 +254,52 @@ def test_same_bits_every_time_and_in_graphs_and_streams(lib, D):
 
 
 @pytest.mark.gpu
+def test_calls_on_several_streams_at_once(lib):
+    """Narrow and wide heads, forward and gradient, side by side on the device: each result is the one of the call alone."""
+    cases = [([700, 300, 64], 4, 2, 64), ([900, 5], 2, 1, 128), ([200] * 20, 3, 3, 32), ([2500], 2, 2, 64)]
+    work = []
+    for i, (lengths, heads, kv_heads, D) in enumerate(cases):
+        qkv, (q, k, v), da = inputs(lengths, heads, kv_heads, D, torch.bfloat16, seed=30 + 2 * i)
+        work.append((q, k, v, da, lib.make_packed_plan(offsets_of(lengths)), heads, kv_heads))
+
+    def step(q, k, v, da, plan, heads, kv_heads):
+        a, lse = lib.elsa_packed_attention(q, k, v, plan, heads, kv_heads, causal=True, want_lse=True)
+        return (a, lse) + lib.elsa_packed_attention_backward(da, q, k, v, a, lse, plan, heads, kv_heads, causal=True)
+
+    alone = [step(*w) for w in work]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in work]
+    for _ in range(10):
+        got = []
+        for s, w in zip(streams, work):
+            with torch.cuda.stream(s):
+                got.append([step(*w) for _ in range(3)])
+        torch.cuda.synchronize()
+        for x, ys in zip(alone, got):
+            for y in ys:
+                assert all(torch.equal(u, w) for u, w in zip(x, y))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D", [64, 128])
+def test_given_stream_and_outputs_of_its_own(lib, D):
+    """stream= without making it current: with rows of no sequence the call's own outputs hold zeros there."""
+    rows, n, heads = 300, 210, 2
+    qkv, (q, k, v), da = inputs([rows], heads, heads, D, torch.float16)
+    side = torch.cuda.Stream()
+    plan = lib.make_packed_plan([20, 20 + n], rows)
+    torch.cuda.synchronize()
+    a, lse = lib.elsa_packed_attention(q, k, v, plan, heads, want_lse=True, stream=side)
+    grads = lib.elsa_packed_attention_backward(da, q, k, v, a, lse, plan, heads, stream=side)
+    side.synchronize()
+    r = slice(20, 20 + n)
+    ref, tol = formula(q[r], k[r], v[r], [n], heads, heads, False, D ** -0.5, da[r])
+    for name, got in zip(("a", "dq", "dk", "dv"), (a,) + grads):
+        near(name, got[r], ref[name], tol[name])
+        assert (got[:20] == 0).all() and (got[20 + n:] == 0).all()
+
+
+@pytest.mark.gpu
 def test_plans_that_do_not_fit(lib):
     """Offsets that are none, and a plan of another batch: nothing is written, dev_status tells."""
     heads, D, rows = 2, 64, 100
