@@ -526,7 +526,7 @@ elsa_status elsa_nm_linear_backward(const void* dY, const void* X, int rows, con
  * video or causal sequences: LayerNorm with its gradient, rotary positions, attention over packed sequences with its
  * gradient.  16-bit tensors of one dtype, fp32 arithmetic, one rounding of each stored value; no atomics on results: the
  * same inputs give the same bits every time.  DEVICE pointers, 16-byte aligned, unless stated otherwise; asynchronous on
- * `stream`; errors as for elsa_nm_linear.  At most 2^30 rows.  Calls that share a workspace must be stream-ordered.
+ * `stream`; errors as for elsa_nm_linear.  At most 2^30 rows and sequences.  Calls that share a workspace must be stream-ordered.
  *
  * LayerNorm of rows of dim values (a multiple of 8):
  *     s = x + residual (rounded to dtype; without a residual s is x)
@@ -580,7 +580,8 @@ elsa_status elsa_rotary(const void* x, long long x_pitch, const int32_t* positio
  *     a[r, h] = sum over j of p_j v[j, h / group],   p = softmax over j of scale * q[r, h] . k[j, h / group]
  * over the rows j of r's own sequence, causal: those up to r; group = heads / kv_heads query heads share a key head.
  * Rows of no sequence are neither read nor written.  Non-finite values of one sequence reach no other; inside a sequence
- * one in v, or in da, may reach every row of it, a causal mask or not.
+ * one in v, or in the gradient one in any input, may reach every row of it, a causal mask or not.  Outputs may not overlap
+ * inputs.
  *
  * elsa_packed_plan cuts the sequences into tiles once for any number of calls with the same offsets (all layers, both
  * directions): plan is elsa_packed_plan_bytes(...) of device memory that the calls read, on any stream ordered behind it; it stays
@@ -609,8 +610,7 @@ elsa_status elsa_packed_attention(const elsa_packed_qkv* in, elsa_dtype dtype, c
 /*
  * The gradient, da arriving at a: dq like q, dk and dv like k and v (rows dq_pitch, dk_pitch, dv_pitch values apart, so
  * they may be the thirds of one tensor), sums over the query heads of a key head included.  a and lse: the forward
- * call's.  workspace: elsa_packed_attention_workspace_bytes(rows, heads) bytes, 256-byte aligned.  Outputs may not overlap
- * inputs.
+ * call's.  workspace: elsa_packed_attention_workspace_bytes(rows, heads) bytes, 256-byte aligned.
  */
 size_t elsa_packed_attention_workspace_bytes(int rows, int heads);
 elsa_status elsa_packed_attention_backward(const elsa_packed_qkv* in, elsa_dtype dtype, const void* plan, int sequences,

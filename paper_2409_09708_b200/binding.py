@@ -535,6 +535,8 @@ def make_packed_plan(offsets, rows=None, device="cuda", dev_status=None, stream=
     int32 tensor on the device, checked there (dev_status); rows: of the tensors, at least the last offset (default: it).  A
     captured call reads the plan at every replay: keep it."""
     full = False
+    if rows is not None and not 0 <= rows < 1 << 31:
+        raise ValueError("rows=%s does not fit an int" % rows)
     if not torch.is_tensor(offsets) or not offsets.is_cuda:
         host = [int(o) for o in (offsets.tolist() if torch.is_tensor(offsets) else offsets)]
         if rows is None and host:
@@ -548,7 +550,8 @@ def make_packed_plan(offsets, rows=None, device="cuda", dev_status=None, stream=
     if offsets.get_device() != torch.cuda.current_device():
         raise ValueError("offsets on %s, the current device is cuda:%d" % (offsets.device, torch.cuda.current_device()))
     nbytes = int(_packed_plan_bytes(rows, offsets.numel() - 1))
-    buffer = torch.empty((max(nbytes, 16),), dtype=torch.uint8, device=offsets.device)
+    with torch.cuda.stream(stream):                                     # None: as it is
+        buffer = torch.empty((max(nbytes, 16),), dtype=torch.uint8, device=offsets.device)
     _check(_packed_plan(_ptr(offsets), offsets.numel() - 1, rows, _ptr(buffer), nbytes, _ptr(dev_status), _stream(stream)))
     return PackedPlan(offsets, rows, full, buffer)
 

@@ -1719,13 +1719,14 @@ int elsa_profile_stop(elsa_kernel_time* records, int capacity)
 unsigned long long elsa_launch_count(void) { return g_launches.load(std::memory_order_relaxed); }
 
 namespace {
-// Rows of the calls below: the kernels step through them in ints.
+// Rows and sequences of the calls below: the kernels step through them in ints.
 constexpr int kMostRows = 1 << 30;
-elsa_status check_rows(int rows)
+elsa_status check_count(const char* name, int n)
 {
-    if (rows <= 0) return fail(ELSA_ERR_SHAPE, "non-positive rows=%d", rows);
-    return rows <= kMostRows ? ELSA_OK : fail(ELSA_ERR_SHAPE, "rows=%d is above 2^30", rows);
+    if (n <= 0) return fail(ELSA_ERR_SHAPE, "non-positive %s=%d", name, n);
+    return n <= kMostRows ? ELSA_OK : fail(ELSA_ERR_SHAPE, "%s=%d is above 2^30", name, n);
 }
+elsa_status check_rows(int rows) { return check_count("rows", rows); }
 }  // namespace
 
 elsa_status elsa_layer_norm(const void* x, const void* residual, const void* gain, const void* bias, int rows, int dim, float eps,
@@ -1784,10 +1785,13 @@ elsa_status elsa_rotary(const void* x, long long x_pitch, const int32_t* positio
     if (plan->head_dim < 16 || plan->head_dim > 2 * ELSA_ROTARY_MAX_PAIRS || plan->head_dim % 16 != 0 || plan->axes < 1 ||
         plan->axes > ELSA_ROTARY_MAX_AXES)
         return fail(ELSA_ERR_SHAPE, "the plan is none that elsa_rotary_make_plan makes (head_dim=%d, axes=%d)", plan->head_dim, plan->axes);
+    for (int pair = 0; pair < plan->head_dim / 2; ++pair)
+        if (plan->axis[pair] >= plan->axes) return fail(ELSA_ERR_SHAPE, "the plan is none that elsa_rotary_make_plan makes (axis of pair %d)", pair);
     elsa_status st = check_rows(rows);
     if (st != ELSA_OK) return st;
     if (heads <= 0) return fail(ELSA_ERR_SHAPE, "non-positive heads=%d", heads);
     const long long width = (long long)heads * plan->head_dim;
+    if (width > 0x7fffffffLL) return fail(ELSA_ERR_SHAPE, "heads * head_dim does not fit an int");
     if (x_pitch < width || y_pitch < width)
         return fail(ELSA_ERR_SHAPE, "x_pitch=%lld and y_pitch=%lld must be at least %d heads * %d", x_pitch, y_pitch, heads, plan->head_dim);
     if (x_pitch % 8 != 0 || y_pitch % 8 != 0) return fail(ELSA_ERR_ALIGN, "x_pitch=%lld and y_pitch=%lld must be multiples of 8", x_pitch, y_pitch);
@@ -1797,14 +1801,17 @@ elsa_status elsa_rotary(const void* x, long long x_pitch, const int32_t* positio
     return launch_rotary((const uint16_t*)x, x_pitch, positions, *plan, rows, heads, inverse != 0, dtype, (uint16_t*)y, y_pitch, (cudaStream_t)stream);
 }
 
-size_t elsa_packed_plan_bytes(int rows, int sequences) { return rows <= 0 || rows > kMostRows || sequences <= 0 ? 0 : packed_plan_bytes(rows, sequences); }
+size_t elsa_packed_plan_bytes(int rows, int sequences)
+{
+    return rows <= 0 || rows > kMostRows || sequences <= 0 || sequences > kMostRows ? 0 : packed_plan_bytes(rows, sequences);
+}
 
 elsa_status elsa_packed_plan(const int32_t* offsets, int sequences, int rows, void* plan, size_t plan_bytes, uint32_t* dev_status, void* stream)
 {
     if (!offsets || !plan) return fail(ELSA_ERR_NULL, "offsets and plan must not be NULL");
     elsa_status st = check_rows(rows);
     if (st != ELSA_OK) return st;
-    if (sequences <= 0) return fail(ELSA_ERR_SHAPE, "non-positive sequences=%d", sequences);
+    if ((st = check_count("sequences", sequences)) != ELSA_OK) return st;
     if (((uintptr_t)offsets & 3u) || !aligned16(plan)) return fail(ELSA_ERR_ALIGN, "offsets must be 4-byte aligned, plan 16-byte aligned");
     const size_t need = packed_plan_bytes(rows, sequences);
     if (plan_bytes < need) return fail(ELSA_ERR_WORKSPACE, "plan of %zu bytes needed, %zu given", need, plan_bytes);
@@ -1825,8 +1832,8 @@ elsa_status check_packed(const elsa_packed_qkv* in, int dtype, const void* plan,
     if (dtype != ELSA_F16 && dtype != ELSA_BF16) return fail(ELSA_ERR_DTYPE, "dtype %d is neither ELSA_F16 nor ELSA_BF16", dtype);
     elsa_status st = check_rows(in->rows);
     if (st != ELSA_OK) return st;
-    if (in->heads <= 0 || in->kv_heads <= 0 || sequences <= 0)
-        return fail(ELSA_ERR_SHAPE, "non-positive dimension (heads=%d, kv_heads=%d, sequences=%d)", in->heads, in->kv_heads, sequences);
+    if ((st = check_count("sequences", sequences)) != ELSA_OK) return st;
+    if (in->heads <= 0 || in->kv_heads <= 0) return fail(ELSA_ERR_SHAPE, "non-positive dimension (heads=%d, kv_heads=%d)", in->heads, in->kv_heads);
     if (in->head_dim != 32 && in->head_dim != 64 && in->head_dim != 128) return fail(ELSA_ERR_SHAPE, "head_dim=%d is neither 32, 64 nor 128", in->head_dim);
     if (in->heads % in->kv_heads != 0) return fail(ELSA_ERR_SHAPE, "heads=%d is not a multiple of kv_heads=%d", in->heads, in->kv_heads);
     if ((long long)in->heads * in->head_dim > 0x7fffffffLL) return fail(ELSA_ERR_SHAPE, "heads * head_dim does not fit an int");

@@ -377,6 +377,12 @@ std::string text(at::IntArrayRef shape)
     return r + "]";
 }
 
+// Rows and columns as ints, which the entry points take; they say what else is too many.
+void sizes_fit(const at::Tensor& t, const char* name)
+{
+    if (t.size(0) > 0x7fffffff || t.size(1) > 0x7fffffff) raise(PyExc_ValueError, "%s: shape %s does not fit an int", name, text(t.sizes()).c_str());
+}
+
 void shape_is(const at::Tensor* t, at::IntArrayRef want, const char* name)
 {
     if (t != nullptr && t->sizes() != want)
@@ -394,6 +400,16 @@ void* address(const at::Tensor* t) { return t == nullptr ? nullptr : pointer(*t)
 
 // The given stream's handle, or the current stream's.
 void* stream_of(PyObject* o) { return o == Py_None ? (void*)c10::cuda::getCurrentCUDAStream().stream() : handle(o); }
+
+// While it lives the given stream is torch's current one, so that what a call allocates belongs to the stream that it runs on: a block of
+// another stream's could still be in use there, and would go back to it while this call runs.
+struct OnStream {
+    c10::cuda::OptionalCUDAStreamGuard guard;
+    OnStream(PyObject* o, const at::Tensor& t)
+    {
+        if (o != Py_None) guard.reset_stream(c10::cuda::getStreamFromExternal((cudaStream_t)handle(o), t.device().index()));
+    }
+};
 
 // A matrix whose rows are contiguous, such as the columns of one third of qkv: its address and the values between rows.
 struct Rows {
@@ -450,7 +466,9 @@ PyObject* layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n)
         const elsa_dtype code = type_code(x);
         same_type(x, {&gain, &bias, residual, y_in, s_in});
         same_place({&x, &gain, &bias, residual, y_in, s_in, stats_in});
+        const OnStream on(a[9], x);
         const int64_t rows = x.size(0), dim = x.size(1);
+        sizes_fit(x, "x");
         shape_is(&gain, {dim}, "gain");
         shape_is(&bias, {dim}, "bias");
         shape_is(residual, {rows, dim}, "residual");
@@ -480,7 +498,9 @@ PyObject* layer_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n)
         const elsa_dtype code = type_code(dy);
         same_type(dy, {&s, &gain, ds, dx_in});
         same_place({&dy, &s, &gain, stats, ds, dx_in, ws_in});
+        const OnStream on(a[10], dy);
         const int64_t rows = dy.size(0), dim = dy.size(1);
+        sizes_fit(dy, "dy");
         shape_is(&s, {rows, dim}, "s");
         shape_is(ds, {rows, dim}, "ds");
         shape_is(dx_in, {rows, dim}, "dx");
@@ -516,7 +536,9 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n)
         same_type(x, {y_in});
         if (positions.scalar_type() != at::kInt) raise(PyExc_TypeError, "positions: int32 expected, got %s%s", c10::toString(positions.scalar_type()), "");
         same_place({&x, &positions, y_in});
+        const OnStream on(a[5], x);
         const int64_t rows = x.size(0), width = x.size(1);
+        sizes_fit(x, "x");
         if (plan == nullptr || plan->head_dim <= 0 || width == 0 || width % plan->head_dim != 0) raise(PyExc_ValueError, "x: its columns are no heads of the plan's%s%s", "", "");
         shape_is(&positions, {rows, plan->axes}, "positions");
         shape_is(y_in, {rows, width}, "y");
@@ -555,6 +577,7 @@ Packed packed_call(PyObject* const* a)
     same_type(q, {&k, &v});
     same_place({&q, &k, &v, p.plan});
     if (heads <= 0 || kv_heads <= 0 || q.size(1) % heads != 0) raise(PyExc_ValueError, "q: its columns are no heads of that number%s%s", "", "");
+    sizes_fit(q, "q");
     const int64_t width = q.size(1) / heads;
     p.wide = q.size(1);
     p.narrow = width * kv_heads;
@@ -567,14 +590,11 @@ Packed packed_call(PyObject* const* a)
     return p;
 }
 
-// Rows of no sequence are left as they are: where there may be some, an output of the call's own starts as zeros, on the call's stream.
-at::Tensor output_rows(const Packed& p, const at::Tensor* given, int64_t width, PyObject* stream)
+// Rows of no sequence are left as they are: where there may be some, an output of the call's own starts as zeros.
+at::Tensor output(const Packed& p, const at::Tensor* given, at::IntArrayRef shape, at::ScalarType type)
 {
     if (given != nullptr) return *given;
-    if (p.full) return fresh(*p.q, {p.rows, width}, p.q->scalar_type());
-    c10::cuda::OptionalCUDAStreamGuard guard;
-    if (stream != Py_None) guard.reset_stream(c10::cuda::getStreamFromExternal((cudaStream_t)handle(stream), p.q->device().index()));
-    return at::zeros({p.rows, width}, p.q->options());
+    return p.full ? fresh(*p.q, shape, type) : at::zeros(shape, p.q->options().dtype(type));
 }
 
 // the eleven of packed_call, a, lse wanted, lse, dev_status, stream -> (a, lse)
@@ -587,10 +607,10 @@ PyObject* packed_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
         same_place({a_in, lse_in, status});
         shape_is(a_in, {p.rows, p.wide}, "a");
         floats(lse_in, {p.in.heads, p.rows}, "lse", false);
-        const at::Tensor out = output_rows(p, a_in, p.wide, a[15]);
+        const OnStream on(a[15], *p.q);
+        const at::Tensor out = output(p, a_in, {p.rows, p.wide}, p.q->scalar_type());
         at::Tensor lse;
-        if (lse_in != nullptr) lse = *lse_in;
-        else if (truth(a[12])) lse = fresh(*p.q, {p.in.heads, p.rows}, at::kFloat);
+        if (lse_in != nullptr || truth(a[12])) lse = output(p, lse_in, {p.in.heads, p.rows}, at::kFloat);
         const Rows ar = rows_of(out, "a");
         void *plan = pointer(*p.plan), *lp = lse.defined() ? pointer(lse) : nullptr, *sp = address(status), *stream = stream_of(a[15]);
         const elsa_status st = unlocked([&] { return g_packed(&p.in, p.code, plan, p.sequences, ar.at, ar.pitch, (float*)lp, (uint32_t*)sp, stream); });
@@ -612,13 +632,14 @@ PyObject* packed_attention_backward(PyObject*, PyObject* const* a, Py_ssize_t n)
         shape_is(&da, {p.rows, p.wide}, "da");
         shape_is(&out, {p.rows, p.wide}, "a");
         floats(lse, {p.in.heads, p.rows}, "lse", true);
+        const OnStream on(a[19], *p.q);
         at::Tensor grad[3];
         Rows g[3];
         static const char* const names[3] = {"dq", "dk", "dv"};
         for (int i = 0; i < 3; ++i) {
             const int64_t width = i == 0 ? p.wide : p.narrow;
             shape_is(grad_in[i], {p.rows, width}, names[i]);
-            grad[i] = output_rows(p, grad_in[i], width, a[19]);
+            grad[i] = output(p, grad_in[i], {p.rows, width}, p.q->scalar_type());
             g[i] = rows_of(grad[i], names[i]);
         }
         const at::Tensor ws = workspace(a[17], *p.q, g_packed_workspace_bytes((int)p.rows, p.in.heads));

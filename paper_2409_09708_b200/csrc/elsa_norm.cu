@@ -28,7 +28,7 @@ struct Group {
 // eight warps whatever the width: 63 and 109).
 constexpr int backward_per_sm(int row_lanes, int vpl)
 {
-    const int warps = vpl == 1 ? 28 : vpl == 2 ? 16 : vpl == 3 ? 8 : 8, cta_warps = row_lanes > 128 ? row_lanes / 32 : 4;
+    const int warps = vpl == 1 ? 28 : vpl == 2 ? 16 : 8, cta_warps = row_lanes > 128 ? row_lanes / 32 : 4;
     return warps / cta_warps < 1 ? 1 : warps / cta_warps;
 }
 

@@ -71,6 +71,10 @@ def test_rotary(lib):
         other = lib.make_rotary_plan(64, [16, 16])
         setattr(other, field, value)
         assert call(plan=ctypes.byref(other)) == SHAPE, field
+    other = lib.make_rotary_plan(64, [16, 16])
+    other.axis[31] = 2
+    assert call(plan=ctypes.byref(other)) == SHAPE
+    assert call(heads=1 << 25, xp=1 << 40, yp=1 << 40) == SHAPE
     assert call(dt=7) == DTYPE
     for kw in (dict(x=FAKE + 8), dict(y=WORK + 2), dict(positions=FAKE + 2), dict(xp=260), dict(yp=257)):
         assert call(**kw) == ALIGN, kw
@@ -81,6 +85,7 @@ def test_packed_plan(lib):
     call = caller(lib._packed_plan, names, dict(offsets=FAKE, sequences=3, rows=500, plan=WORK, bytes=1 << 20, status=None, stream=None))
     assert call(offsets=None) == NULL and call(plan=None) == NULL
     assert call(sequences=0) == SHAPE and call(rows=0) == SHAPE and call(rows=(1 << 30) + 1) == SHAPE
+    assert call(sequences=(1 << 30) + 1) == SHAPE and lib._packed_plan_bytes(5, (1 << 30) + 1) == 0
     assert call(offsets=FAKE + 2) == ALIGN and call(plan=WORK + 8) == ALIGN
     need = int(lib._packed_plan_bytes(500, 3))
     assert need == 64 + 16 * ((500 // 128 + 3) + (500 // 256 + 3)) and call(bytes=need - 1) == WORKSPACE
@@ -91,6 +96,9 @@ def test_packed_plan(lib):
             lib.make_packed_plan(bad)
     with pytest.raises(ValueError):
         lib.make_packed_plan([0, 5], rows=4)
+    for rows in (-1, 1 << 31, (1 << 32) + 5):
+        with pytest.raises(ValueError):
+            lib.make_packed_plan([0, 5], rows=rows)
 
 
 def qkv_of(lib, **kw):
@@ -111,7 +119,7 @@ def test_packed_attention(lib):
     for kw, want in COMMON:
         assert call(qkv=qkv_of(lib, **kw)) == want, kw
     assert call(qkv=None) == NULL and call(plan=None) == NULL and call(a=None) == NULL
-    assert call(sequences=0) == SHAPE and call(ap=255) == SHAPE
+    assert call(sequences=0) == SHAPE and call(sequences=(1 << 30) + 1) == SHAPE and call(ap=255) == SHAPE
     assert call(dt=9) == DTYPE
     assert call(plan=FAKE + 4) == ALIGN and call(a=WORK + 2) == ALIGN and call(ap=257) == ALIGN and call(lse=FAKE + 2) == ALIGN
 
@@ -184,3 +192,17 @@ def test_tensors_of_the_wrong_shape(lib):
         with pytest.raises(ValueError):
             lib.make_packed_plan(bad, 4)
     assert lib.elsa_packed_attention(x, x, x, packed, 2)[1] is None
+
+
+@pytest.mark.gpu
+def test_sizes_that_fit_no_int(lib):
+    """More rows than an int counts (expanded, so that they take no memory) are refused before anything is cut short."""
+    x = torch.zeros(1, 64, dtype=torch.float16, device="cuda").expand((1 << 32) + 4, 64)
+    g = torch.zeros(64, dtype=torch.float16, device="cuda")
+    stats = torch.zeros(1, 2, device="cuda").expand(x.shape[0], 2)
+    at = torch.zeros(1, 1, dtype=torch.int32, device="cuda").expand(x.shape[0], 1)
+    packed = lib.make_packed_plan([0, 4])
+    for bad in (lambda: lib.elsa_layer_norm(x, g, g, y=x), lambda: lib.elsa_layer_norm_backward(x, x, g, stats, dx=x),
+                lambda: lib.elsa_rotary(x, at, lib.make_rotary_plan(64, [32]), y=x), lambda: lib.elsa_packed_attention(x, x, x, packed, 1)):
+        with pytest.raises(ValueError, match="int"):
+            bad()

@@ -300,6 +300,46 @@ def test_given_stream_and_outputs_of_its_own(lib, D):
 
 
 @pytest.mark.gpu
+def test_memory_of_a_call_belongs_to_its_stream(lib):
+    """A call on a stream that is not current, while the current one has writes to freed blocks before it: what the call allocates is
+    neither such a block nor goes back to that stream while the call runs."""
+    lengths, heads, D = [512, 300], 4, 64
+    qkv, (q, k, v), da = inputs(lengths, heads, heads, D, torch.float16)
+    rows = sum(lengths)
+    x = da.contiguous()
+    gain = torch.ones(heads * D, dtype=torch.float16, device="cuda")
+    side = torch.cuda.Stream()
+    plan = lib.make_packed_plan(offsets_of(lengths))
+    offsets = torch.tensor(offsets_of(lengths), dtype=torch.int32, device="cuda")
+
+    def step(stream):
+        another = lib.make_packed_plan(offsets, rows, stream=stream)
+        b, _ = lib.elsa_packed_attention(q, k, v, another, heads, causal=True, stream=stream)
+        a, lse = lib.elsa_packed_attention(q, k, v, plan, heads, want_lse=True, stream=stream)
+        y, _, stats = lib.elsa_layer_norm(x, gain, gain, want_stats=True, stream=stream)
+        return (a, b, lse, y, stats) + lib.elsa_packed_attention_backward(da, q, k, v, a, lse, plan, heads, stream=stream) + \
+            lib.elsa_layer_norm_backward(x, x, gain, stats, stream=stream)
+
+    ref = step(None)
+    torch.cuda.synchronize()
+    sizes = [t.numel() * t.element_size() for t in ref] + [1 << 20, 1 << 16, 1 << 12]
+    freed = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(4)]
+    torch.cuda._sleep(50_000_000)
+    for t in freed:
+        t.fill_(0x7f)
+    del freed, t
+    got = step(side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(u, w) for u, w in zip(ref, got))
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(50_000_000)
+    got = step(side)
+    others = [torch.empty(n, dtype=torch.uint8, device="cuda").fill_(0x7f) for n in sizes for _ in range(4)]       # on the current stream
+    torch.cuda.synchronize()
+    assert len(others) > 0 and all(torch.equal(u, w) for u, w in zip(ref, got))
+
+
+@pytest.mark.gpu
 def test_plans_that_do_not_fit(lib):
     """Offsets that are none, and a plan of another batch: nothing is written, dev_status tells."""
     heads, D, rows = 2, 64, 100
