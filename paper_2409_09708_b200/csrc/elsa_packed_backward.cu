@@ -33,7 +33,7 @@ constexpr int kWalk = 64;                // walked rows of a tile
 // with 8 heads 193 and 176; dk and dv of 64 images of 49 to 1024 rows 228 and 240, of 16 x 1024 164 and 150, of 2 x 4736 228 and 193).
 constexpr int kLongForQueries = 2048, kLongForKeys = 768;
 
-template <int kD, int kGroupsOf>
+template <int kD, bool kKeys, int kGroupsOf>
 struct BackwardShape {
     static constexpr int kGroups = kGroupsOf;
     static constexpr int kPerSm = kGroups == 1 ? 2 : 1;
@@ -42,6 +42,7 @@ struct BackwardShape {
     static constexpr int kTmemCols = 512 / kPerSm;
     static constexpr int kKeptBytes = TileShape<kD>::bytes(128), kWalkBytes = TileShape<kD>::bytes(kWalk);
     static constexpr int kAcc1 = 128 * kGroups, kAcc2 = kAcc1 + kD;  // tensor-memory columns; stage g: S at 128 g, T at 128 g + 64
+    static constexpr int kX1 = kAcc1, kX2 = kAcc1 + kD / 2;          // in the first kernel, which has no acc1
     static_assert(kAcc2 + kD <= kTmemCols, "tensor memory");
     static constexpr int kVectorBytes = 2 * kWalk * 4;               // -lse log2(e), -delta
     static constexpr int kSmemBytes = 2 * kKeptBytes + kRing * (2 * kWalkBytes + kVectorBytes) + 1024 /* alignment */ + 256 /* barriers */;
@@ -77,10 +78,84 @@ __device__ __forceinline__ void copies_arrive(uint32_t bar)
     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
 
-template <bool kBf16, int kD, bool kKeys, int kGroupsOf>
-__global__ void __launch_bounds__(BackwardShape<kD, kGroupsOf>::kThreads, BackwardShape<kD, kGroupsOf>::kPerSm) packed_attention_backward_kernel(const __grid_constant__ BackwardParams p)
+// A lane's row of a kept tile, as TMA laid it in shared memory, to tensor memory as an A operand: 16 columns of the head in 8 words.
+template <int kD>
+__device__ __forceinline__ void keep_rows(uint32_t tile, uint32_t t_lane, int row)
 {
-    using B = BackwardShape<kD, kGroupsOf>;
+    using T = TileShape<kD>;
+    const int sw = T::kRowBytes == 128 ? row & 7 : (row >> 1) & 3;
+#pragma unroll
+    for (int c = 0; c < kD / 2; c += 16) {
+        uint32_t x[16];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const int at = c / 4 + v, half = at / (T::kCols / 8), vec = at % (T::kCols / 8);       // 16 bytes each
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[4 * v]), "=r"(x[4 * v + 1]), "=r"(x[4 * v + 2]), "=r"(x[4 * v + 3])
+                         : "r"(tile + (uint32_t)(half * T::half_bytes(128) + row * T::kRowBytes + (vec ^ sw) * 16)) : "memory");
+        }
+        tmem_st_32x32b_x16(t_lane + (uint32_t)c, x);
+    }
+}
+
+// Lane r: sum over a head's columns of x y in row r of the first rows_left of 32 rows (0 in the others).  A row is read by kD / 8 neighbouring
+// lanes: with a row a lane each load touched 32 lines, and the kernel's beginning took longer than ten of its tiles
+// (8192 rows, 16 heads of 128, causal: 350 to 387 us, by what the first-level cache kept).  begin() asks for the first rows, or for all of narrow
+// heads, sums() waits for them.
+template <bool kBf16, int kD>
+struct RowProducts {
+    static constexpr int kLanes = kD / 8, kRows = 32 / kLanes;       // lanes of a row, rows of a load
+    static constexpr int kAhead = kLanes < 8 ? kLanes : 8;
+    uint4 u[kAhead], w[kAhead];
+    const uint16_t *x, *y;
+    long long x_pitch, y_pitch;
+    int rows_left, lane;
+
+    __device__ __forceinline__ static uint4 load(const uint16_t* row, bool in, int sub)
+    {
+        uint4 r = make_uint4(0u, 0u, 0u, 0u);
+        // in its place: the loads are to be on their way while the warp waits for something else
+        if (in)
+            asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(reinterpret_cast<const uint4*>(row) + sub));
+        return r;
+    }
+    __device__ __forceinline__ void begin(int i0 = 0)
+    {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int r = (i0 + i) * kRows + lane / kLanes;
+            u[i] = load(x + (long long)r * x_pitch, r < rows_left, lane % kLanes);
+            w[i] = load(y + (long long)r * y_pitch, r < rows_left, lane % kLanes);
+        }
+    }
+    __device__ __forceinline__ float sums()
+    {
+        float mine = 0.f;
+#pragma unroll
+        for (int i0 = 0; i0 < kLanes; i0 += kAhead) {
+            if (i0 > 0) begin(i0);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const uint32_t us[4] = {u[i].x, u[i].y, u[i].z, u[i].w}, ws[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+                float part = 0.f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float2 a = raw2_to_float2<kBf16>(us[e]), b = raw2_to_float2<kBf16>(ws[e]);
+                    part = fmaf(a.x, b.x, fmaf(a.y, b.y, part));
+                }
+#pragma unroll
+                for (int o = kLanes / 2; o > 0; o >>= 1) part += __shfl_xor_sync(0xFFFFFFFFu, part, o);
+                const float got = __shfl_sync(0xFFFFFFFFu, part, lane % kRows * kLanes);
+                if (lane / kRows == i0 + i) mine = got;
+            }
+        }
+        return mine;
+    }
+};
+
+template <bool kBf16, int kD, bool kKeys, int kGroupsOf>
+__global__ void __launch_bounds__(BackwardShape<kD, kKeys, kGroupsOf>::kThreads, BackwardShape<kD, kKeys, kGroupsOf>::kPerSm) packed_attention_backward_kernel(const __grid_constant__ BackwardParams p)
+{
+    using B = BackwardShape<kD, kKeys, kGroupsOf>;
     pdl_wait_for_predecessors();
     pdl_release_successors();
     const int kept_heads = kKeys ? p.kv_heads : p.heads;
@@ -98,7 +173,7 @@ __global__ void __launch_bounds__(BackwardShape<kD, kGroupsOf>::kThreads, Backwa
     auto y2_smem = [&](int s) { return y1_smem(s) + (uint32_t)B::kWalkBytes; };
     const uint32_t vectors = smem_base + (uint32_t)(2 * B::kKeptBytes + 2 * B::kRing * B::kWalkBytes);
     const uint32_t bars = vectors + B::kRing * B::kVectorBytes;
-    enum { kXFull = 0, kYFull = 1, kYEmpty = kYFull + B::kRing, kSFull = kYEmpty + B::kRing, kPFull = kSFull + B::kGroups, kDone = kPFull + B::kGroups, kBars };
+    enum { kXFull = 0, kXMoved = 1, kYFull = 2, kYEmpty = kYFull + B::kRing, kSFull = kYEmpty + B::kRing, kPFull = kSFull + B::kGroups, kDone = kPFull + B::kGroups, kBars };
     auto bar = [&](int which, int i) { return bars + (uint32_t)(8 * (which + i)); };
     const uint32_t tmem_holder_addr = bars + 8 * kBars;
     uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(smem_raw + (tmem_holder_addr - smem_u32(smem_raw)));
@@ -115,6 +190,7 @@ __global__ void __launch_bounds__(BackwardShape<kD, kGroupsOf>::kThreads, Backwa
     if (warp == kMmaWarp) {
         if (lane == 0) {
             mbar_init(bar(kXFull, 0), 1);
+            mbar_init(bar(kXMoved, 0), kGroups > 1 ? 8 : 4);
             for (int s = 0; s < kRing; ++s) {
                 mbar_init(bar(kYFull, s), kKeys ? 33 : 1);
                 mbar_init(bar(kYEmpty, s), 1);
@@ -191,6 +267,16 @@ __global__ void __launch_bounds__(BackwardShape<kD, kGroupsOf>::kThreads, Backwa
         auto scores = [&](int u, uint32_t y_round) {
             const int g = u % kGroups;
             const uint32_t t_s = tmem_u + (uint32_t)(128 * g), y_at = y1_rows + y_round + (uint32_t)(u * 2) * kY2;
+            if constexpr (!kKeys) {
+#pragma unroll
+                for (int k = 0; k < kD / 16; ++k)
+                    umma_f16_ts_if(t_s, tmem_u + (uint32_t)(B::kX1 + 8 * k), Desc::of(y_at + Desc::k_step(kWalk, k)), p.idesc_s, (uint32_t)(k != 0), elected);
+#pragma unroll
+                for (int k = 0; k < kD / 16; ++k)
+                    umma_f16_ts_if(t_s + 64, tmem_u + (uint32_t)(B::kX2 + 8 * k), Desc::of(y_at + kY2 + Desc::k_step(kWalk, k)), p.idesc_s, (uint32_t)(k != 0), elected);
+                umma_commit_if(bar(kSFull, g), elected);
+                return;
+            }
 #pragma unroll
             for (int k = 0; k < kD / 16; ++k)
                 umma_f16_if(t_s, Desc::of(x1_desc + Desc::k_step(128, k)), Desc::of(y_at + Desc::k_step(kWalk, k)), p.idesc_s, (uint32_t)(k != 0), elected);
@@ -228,7 +314,7 @@ __global__ void __launch_bounds__(BackwardShape<kD, kGroupsOf>::kThreads, Backwa
         const int last_left = first_left - (tiles_a_head - 1) * kWalk;
         const int last_steps = last_left >= kWalk ? kWalk / 16 : (last_left + 15) / 16;
         int to_last = tiles_a_head, sums_to_last = tiles_a_head;
-        wait(bar(kXFull, 0), 0, 81);
+        if (wait(bar(kKeys ? kXFull : kXMoved, 0), 0, 81)) tc_fence_after();
         uint32_t half = 0, ring_phase = 0;                           // half of the ring, phase of its barriers
         for (int it0 = 0; ok && it0 < tiles + kBehind; it0 += kHalf) {
             const uint32_t y_round = half != 0 ? kRound : 0u, y_before = kRound - y_round;
@@ -279,25 +365,26 @@ __global__ void __launch_bounds__(BackwardShape<kD, kGroupsOf>::kThreads, Backwa
         const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16);
         float minus_lse = 0.f, minus_delta = 0.f;
         if constexpr (!kKeys) {
-            // delta, by each group for itself: an exchange would be one more wait, and the rows are in the first-level cache
+            // delta, by each group for itself: an exchange would be one more wait, and the rows are in the caches
+            RowProducts<kBf16, kD> delta;
+            delta.x = p.a + (long long)(tile.begin + row0) * p.a_pitch + head * kD;
+            delta.y = p.da + (long long)(tile.begin + row0) * p.da_pitch + head * kD;
+            delta.x_pitch = p.a_pitch; delta.y_pitch = p.da_pitch; delta.rows_left = tile.len - row0; delta.lane = lane;
+            delta.begin();
+            const float lse = exists ? __ldg(p.lse + (size_t)head * (size_t)p.rows + (size_t)(tile.begin + row)) : 0.f;
+            // X1 and X2 to tensor memory, a row a lane, by the first group and the second (or one after the other)
+            if (g < 2 && wait(bar(kXFull, 0), 0, 87)) {
+                if (g == 0) keep_rows<kD>(x1_smem, t_lane + B::kX1, 32 * quarter + lane);
+                if (g == (kGroups > 1 ? 1 : 0)) keep_rows<kD>(x2_smem, t_lane + B::kX2, 32 * quarter + lane);
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(kXMoved, 0));
+            }
+            minus_delta = -delta.sums();
             if (exists) {
                 const size_t at = (size_t)head * (size_t)p.rows + (size_t)(tile.begin + row);
-                const uint4* a4 = reinterpret_cast<const uint4*>(p.a + (long long)(tile.begin + row) * p.a_pitch + head * kD);
-                const uint4* d4 = reinterpret_cast<const uint4*>(p.da + (long long)(tile.begin + row) * p.da_pitch + head * kD);
-                const float lse = __ldg(p.lse + at);
-                float part = 0.f;
-#pragma unroll
-                for (int v = 0; v < kD / 8; ++v) {
-                    const uint4 x = __ldg(a4 + v), y = __ldg(d4 + v);
-                    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float2 u = raw2_to_float2<kBf16>(xs[e]), w = raw2_to_float2<kBf16>(ys[e]);
-                        part = fmaf(u.x, w.x, fmaf(u.y, w.y, part));
-                    }
-                }
                 minus_lse = -1.4426950408889634f * lse;
-                minus_delta = -part;
                 if (g == 0) {
                     p.minus_lse[at] = minus_lse;
                     if (n > 1) p.minus_delta[at] = minus_delta;
@@ -422,7 +509,7 @@ __global__ void __launch_bounds__(BackwardShape<kD, kGroupsOf>::kThreads, Backwa
 template <bool kBf16, int kD, bool kKeys, int kGroupsOf>
 elsa_status launch(const BackwardParams& p, cudaStream_t stream, const DeviceInfo& dev)
 {
-    using B = BackwardShape<kD, kGroupsOf>;
+    using B = BackwardShape<kD, kKeys, kGroupsOf>;
     static_assert(2 * B::kRing * B::kWalkBytes >= 4 * B::kGroups * 32 * 2 * TileShape<kD>::kCols, "staging room");
     auto kernel = packed_attention_backward_kernel<kBf16, kD, kKeys, kGroupsOf>;
     static std::atomic<bool> attr_set[64];
