@@ -307,12 +307,23 @@ packed_attention_kernel(const __grid_constant__ ForwardParams p)
                         tmem_st_32x32b_x16(t_lane + (uint32_t)(c0 / 2), reinterpret_cast<const uint32_t(&)[16]>(w));
                     }
                 };
+                // nothing of the chunk takes part in any of the warp's rows
+                auto hide = [&](int c0) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) w[i] = 0u;
+#pragma unroll
+                    for (int c = 0; c < F::kChunk / 2; c += 16) tmem_st_32x32b_x16(t_lane + (uint32_t)(c0 / 2 + c), w);
+                };
                 if (whole) {
 #pragma unroll
                     for (int c0 = 0; c0 < kKeys; c0 += F::kChunk) chunk(std::false_type{}, c0);
                 } else {
 #pragma unroll 1
-                    for (int c0 = 0; c0 < kKeys; c0 += F::kChunk) chunk(std::true_type{}, c0);
+                    for (int c0 = 0; c0 < kKeys; c0 += F::kChunk) {
+                        if (j + c0 > 0 && __all_sync(0xFFFFFFFFu, lim <= c0)) hide(c0);
+                        else chunk(std::true_type{}, c0);
+                    }
                 }
                 tmem_wait_st();
             }

@@ -459,12 +459,23 @@ __global__ void __launch_bounds__(BackwardShape<kD, kKeys, kGroupsOf>::kThreads,
                     if constexpr (kKeys) tmem_st_32x32b_x16(t_lane + (uint32_t)(128 * g + 16 * u), wp);
                     tmem_st_32x32b_x16(t_lane + (uint32_t)(128 * g + 64 + 16 * u), wd);
                 };
-                if (whole) {
+                // no sum reads columns behind the last 16 with a walked row, and nothing is worked out where no row of the warp takes part
+                auto hide = [&](int u) {
+                    uint32_t w[16];
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) unit(std::false_type{}, u);
+                    for (int i = 0; i < 16; ++i) w[i] = 0u;
+                    if constexpr (kKeys) tmem_st_32x32b_x16(t_lane + (uint32_t)(128 * g + 16 * u), w);
+                    tmem_st_32x32b_x16(t_lane + (uint32_t)(128 * g + 64 + 16 * u), w);
+                };
+                if (whole) {
+                    unit(std::false_type{}, 0);
+                    if (tile.len - walked > 32) unit(std::false_type{}, 1);
                 } else {
 #pragma unroll 1
-                    for (int u = 0; u < 2; ++u) unit(std::true_type{}, u);
+                    for (int u = 0; u < 2 && 32 * u < tile.len - walked; ++u) {
+                        if (__all_sync(0xFFFFFFFFu, lo >= 32 * u + 32 || hi <= 32 * u)) hide(u);
+                        else unit(std::true_type{}, u);
+                    }
                 }
                 tmem_wait_st();
             }
