@@ -4,20 +4,26 @@
 // query heads may share a key head.
 //
 // Work item = (tile of query rows of one sequence, head); the tiles come from the caller's plan, longest sequences first, and the
-// hardware hands them to the SMs as they come free.  An item walks its sequence's keys in tiles of 128 with the running-reference
+// hardware hands them to the SMs as they come free.  An item walks its sequence's keys in tiles with the running-reference
 // form of the softmax, so scores never leave the SM:
-//   1. TMA brings the Q tile once and K and V tiles through rings of two stages.
-//   2. S = Q K^T on tcgen05 into 128 fp32 columns of tensor memory.
-//   3. Four warps, one query row a lane: p = 2^(s scale log2(e) - ref), summed in fp32, rounded to the 16-bit type and written to
-//      tensor memory as the A operand.  ref is a whole number at or below the row's maximum so far; where the probabilities of 32 keys
-//      sum to more than 2^15 it is raised, and the sum, the tile's P and O are multiplied by the power of two between the two, which
-//      changes no mantissa.  So there is no pass for the maximum, and no product that only rescales O.
-//   4. O += P V, A from tensor memory, V as it lies in memory.  The rows of V behind a sequence's end (another sequence's, or
-//      nobody's) are zeroed in shared memory first: their probabilities are zero, but zero times NaN is not.
-// What bounds it is the exponentials: 128 x 128 scores cost the special-function unit 1024 cycles, the two products 512 (64 columns)
-// or 1024 (128).  Heads of up to 64 columns: 128 query rows an item and two CTAs on an SM, one's softmax under the other's
-// products.  Heads of 128: K and V tiles are twice as large, so one CTA has 256 query rows, two groups of softmax warps that take
-// turns with the tensor core; P lies over S there, or tensor memory would not hold both tiles' S and O.
+//   1. TMA brings the Q tile and the first K tile, then one stage of two at a time: V of a tile and K of the next, for which the
+//      products of one step ask together.
+//   2. S = Q K^T on tcgen05 into fp32 columns of tensor memory.
+//   3. Four warps, one query row a lane: p = 2^(s scale log2(e) - ref), summed in fp32, rounded to the 16-bit type and written over the
+//      scores it came from as the A operand.  ref is a whole number at or below the row's maximum so far; where the probabilities of a
+//      chunk sum to more than 2^15 it is raised, and the sum, the tile's P and O are multiplied by the power of two between the two, which
+//      changes no mantissa.  So there is no pass for the maximum, and no product that only rescales O.  The tensor core takes P in
+//      the inputs' type: an error of half a step a probability, about as much in the output as its own rounding.
+//   4. O += P V, A from tensor memory, V as it lies in memory, and the next tile's S into the place of this P.  The rows of V behind a
+//      sequence's end (another sequence's, or nobody's) are zeroed in shared memory first: their probabilities are zero, but zero times
+//      NaN is not.
+// Tensor memory sets the tiles.  Heads of up to 64 columns: S of 64 keys and O are 128 columns, so four CTAs of 128 query rows share an
+// SM, each waiting in its turn (16 x 1024 rows of 12 heads: two CTAs with 128 keys 122 us, the first form of four 99, now 75).  Heads of 128: S
+// of 128 keys and O are 256 columns, one CTA has two query tiles whose warps take turns with the tensor core (2 x 4096 rows of 8 heads: forms
+// with 64 keys 152 to 260 us, the first of this 127, now 120).  What bounds it: the special-function unit's 16 exponentials a clock, 512
+// cycles for 128 x 64 scores.  The loop of narrow heads took 622 of them when 2 x 4736 rows of 8 heads took 132 us; they take 123 to 125 now (740
+// TFLOP/s).  With 128 columns products of 1024 cycles for 128 x 128 scores come on top, and the two tiles' waits for them
+// (8192 causal rows of 16 heads: 1.26 PFLOP/s, less at the power limit, where the clock falls from 1.96 to 1.65 GHz).
 #include <atomic>
 #include <type_traits>
 

@@ -12,11 +12,15 @@
 //     T  = X2 Y2^T                                               da v^T           v da^T
 //     acc2 += ds Y1  (ds rounded to the 16-bit type)             ds k             ds^T q
 //     acc1 += p Y2   (p rounded to the 16-bit type)              -                p^T da
-// All products run on tcgen05; S and T go to fp32 columns of tensor memory, p and ds come back over them as A operands.  Two stages of
-// S and T, each with its own four warps (a row a lane): one stage's exponentials run under the other's products.
-// In the second kernel lse and delta belong to the walked rows: they come with each tile into shared memory.
-// What bounds it: per tile 512 cycles of exponentials, and products of 640 (384) cycles for heads of 64 columns, 1280 (1024) for 128:
-// the shared memory's 128 bytes a cycle bound S and T (6 KB for each 16 columns of the head, 48 cycles against the tensor core's 32).
+// All products run on tcgen05; S and T go to fp32 columns of tensor memory, p and ds come back over them as A operands.  A stage of
+// S and T has four warps of its own (a row a lane): one stage's exponentials run under the others' products.
+// The dq kernel has room in tensor memory for X1 and X2 too: a product of 64 columns with A there takes 32 cycles, with A in shared
+// memory 48, for its 6 KB at 128 bytes a cycle (dq of 16 x 1024 rows of 12 heads of 64: 146 and 129 us).
+// In the dk, dv kernel lse and delta belong to the walked rows: they come with each tile into shared memory.
+// What bounds it is the chain of a tile (S and T, a stage's exponentials, the sums) with as few stages under one another as tensor
+// memory holds: a tile of long sequences takes 930 (dq) and 1150 cycles (dk, dv) for heads of 64 columns, where the exponentials
+// take 512 and the products 384 and 640; 1340 and 1680 for heads of 128, products 768 and 1280.  Parts of 32 walked rows with twice the stages
+// are slower (148 to 165 and 183 to 237 us for 2 x 4736 rows of 8 heads of 64): as many products again to issue.
 #include <atomic>
 #include <type_traits>
 
@@ -27,10 +31,10 @@ namespace {
 
 constexpr int kWalk = 64;                // walked rows of a tile
 
-// kGroups: stages of S and T, each with four warps.  Heads of 128 columns have two of them on an SM.  Narrower heads have one in each of two
+// kGroups: stages of S and T.  Heads of 128 columns have two of them on an SM.  Narrower heads have one in each of two
 // CTAs, where one's beginning and end run under the other's products, or three in one, which keep the tensor core busier once they
-// run: chosen by the sequences' mean length (12 heads of 64, us with one and with three: dq of 16 x 1024 rows 146 and 162, of 2 x 4736
-// with 8 heads 193 and 176; dk and dv of 64 images of 49 to 1024 rows 228 and 240, of 16 x 1024 164 and 150, of 2 x 4736 228 and 193).
+// run: chosen by the sequences' mean length (12 heads of 64, us with one and with three: dq of 64 images of 49 to 1024 rows 191 and 224,
+// of 16 x 1024 132 and 136, of 6 x 2048 158 and 154; dk and dv of the images 230 and 240, of 32 x 512 97 and 101, of 16 x 1024 166 and 154).
 constexpr int kLongForQueries = 2048, kLongForKeys = 768;
 
 template <int kD, bool kKeys, int kGroupsOf>
@@ -99,7 +103,7 @@ __device__ __forceinline__ void keep_rows(uint32_t tile, uint32_t t_lane, int ro
 
 // Lane r: sum over a head's columns of x y in row r of the first rows_left of 32 rows (0 in the others).  A row is read by kD / 8 neighbouring
 // lanes: with a row a lane each load touched 32 lines, and the kernel's beginning took longer than ten of its tiles
-// (8192 rows, 16 heads of 128, causal: 350 to 387 us, by what the first-level cache kept).  begin() asks for the first rows, or for all of narrow
+// (8192 rows, 16 heads of 128, causal: 350 to 387 us, by what the first-level cache kept; 331 so).  begin() asks for the first rows, or for all of narrow
 // heads, sums() waits for them.
 template <bool kBf16, int kD>
 struct RowProducts {
@@ -358,7 +362,7 @@ __global__ void __launch_bounds__(BackwardShape<kD, kKeys, kGroupsOf>::kThreads,
         }
         __syncwarp();
     } else {
-        // ------------------------------------------------ p and ds, then the sums' way out: group g takes the tiles g, g + 2, ...
+        // ------------------------------------------------ p and ds, then the sums' way out: group g takes the tiles g, g + kGroups, ...
         const int g = warp >> 2, quarter = warp & 3;
         const int row0 = tile.first + 32 * quarter, row = row0 + lane;                 // kept row, in the sequence
         const bool exists = row < tile.len;
