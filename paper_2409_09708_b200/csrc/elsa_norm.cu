@@ -149,8 +149,13 @@ layer_norm_backward_kernel(const uint16_t* dY, const uint16_t* __restrict__ S, c
     const int vecs = dim >> 3;
     const float inv_dim = 1.0f / (float)dim;
     const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-    uint4 x[kVpl], d[kVpl], r[kAdd ? kVpl : 1], gn[kVpl];
-    float2 st = make_float2(0.f, 0.f);
+    // rows on their way: two where the registers of a lane hold them
+    constexpr int kAhead = kVpl == 3 && kRowWarps <= 8 ? 2 : 1;
+    struct Row {
+        uint4 x[kVpl], d[kVpl], r[kAdd ? kVpl : 1];
+        float2 st;
+    } ahead[kAhead];
+    uint4 gn[kVpl];
     // rows of more than 8192 values: 512 threads leave no registers for the sums, and one row group has the shared memory for itself
     constexpr bool kSharedSums = kRowWarps > 8;
     float dgain[kSharedSums ? 1 : kVpl][8], dbias[kSharedSums ? 1 : kVpl][8];
@@ -165,34 +170,35 @@ layer_norm_backward_kernel(const uint16_t* dY, const uint16_t* __restrict__ S, c
             else if (partial != nullptr && v < vecs) columns[8 * v + e] = columns[dim + 8 * v + e] = 0.f;
         }
     }
-    auto load = [&](int row) {
-        st = row < rows ? __ldg(stats + row) : make_float2(0.f, 0.f);
+    auto load = [&](Row& a, int row) {
+        a.st = row < rows ? __ldg(stats + row) : make_float2(0.f, 0.f);
 #pragma unroll
         for (int c = 0; c < kVpl; ++c) {
             const int v = sub + G::kRowLanes * c;
             const bool in = row < rows && v < vecs;
             const size_t at = (size_t)row * (size_t)dim;
-            x[c] = in ? __ldg(reinterpret_cast<const uint4*>(S + at) + v) : zero;
-            d[c] = in ? reinterpret_cast<const uint4*>(dY + at)[v] : zero;
-            if constexpr (kAdd) r[c] = in ? reinterpret_cast<const uint4*>(dS + at)[v] : zero;
+            a.x[c] = in ? __ldg(reinterpret_cast<const uint4*>(S + at) + v) : zero;
+            a.d[c] = in ? reinterpret_cast<const uint4*>(dY + at)[v] : zero;
+            if constexpr (kAdd) a.r[c] = in ? reinterpret_cast<const uint4*>(dS + at)[v] : zero;
         }
     };
     const int stride = gridDim.x * G::kGroups;
     const int steps = (rows - blockIdx.x * G::kGroups + stride - 1) / stride;
     int row = blockIdx.x * G::kGroups + group;
-    load(row);
-    for (int step = 0; step < steps; ++step, row += stride) {
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) load(ahead[a], row + a * stride);
+    auto one_row = [&](Row& a) {
         float xhat[kVpl][8], g[kVpl][8];
         uint4 rr[kAdd ? kVpl : 1];
         float2 t = make_float2(0.f, 0.f);
-        const float rstd = st.y;
+        const float rstd = a.st.y, mean = a.st.x;
 #pragma unroll
         for (int c = 0; c < kVpl; ++c) {
             float gv[8];
-            unpack8<kBf16>(x[c], xhat[c]);
-            unpack8<kBf16>(d[c], g[c]);
+            unpack8<kBf16>(a.x[c], xhat[c]);
+            unpack8<kBf16>(a.d[c], g[c]);
             unpack8<kBf16>(gn[c], gv);
-            if constexpr (kAdd) rr[c] = r[c];
+            if constexpr (kAdd) rr[c] = a.r[c];
             const int v = sub + G::kRowLanes * c;
             float4* sum4 = reinterpret_cast<float4*>(columns + 8 * v);
             float had[2][8];
@@ -205,7 +211,7 @@ layer_norm_backward_kernel(const uint16_t* dY, const uint16_t* __restrict__ S, c
             // columns past the row's end and rows past the last have dy = 0 and a mean and rstd that are finite: they add nothing
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                xhat[c][e] = (xhat[c][e] - st.x) * rstd;
+                xhat[c][e] = (xhat[c][e] - mean) * rstd;
                 if constexpr (kSharedSums) {
                     had[0][e] += g[c][e] * xhat[c][e];
                     had[1][e] += g[c][e];
@@ -224,19 +230,26 @@ layer_norm_backward_kernel(const uint16_t* dY, const uint16_t* __restrict__ S, c
                 }
             }
         }
-        load(row + stride);
+        load(a, row + kAhead * stride);
         const float2 m = row_sums<G, kLanes, kRowWarps>(t, sums, turn);
-        if (dX == nullptr || row >= rows) continue;
+        if (dX == nullptr || row >= rows) return;
         const float c1 = m.x * inv_dim, c2 = m.y * inv_dim;
 #pragma unroll
         for (int c = 0; c < kVpl; ++c) {
             const int v = sub + G::kRowLanes * c;
             if (v >= vecs) continue;
-            float a[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if constexpr (kAdd) unpack8<kBf16>(rr[c], a);
+            float out[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if constexpr (kAdd) unpack8<kBf16>(rr[c], out);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) a[e] += rstd * (g[c][e] - c1 - xhat[c][e] * c2);
-            reinterpret_cast<uint4*>(dX + (size_t)row * (size_t)dim)[v] = pack8<kBf16>(a);
+            for (int e = 0; e < 8; ++e) out[e] += rstd * (g[c][e] - c1 - xhat[c][e] * c2);
+            reinterpret_cast<uint4*>(dX + (size_t)row * (size_t)dim)[v] = pack8<kBf16>(out);
+        }
+    };
+    for (int step = 0; step < steps; step += kAhead) {
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+            if (step + a < steps) one_row(ahead[a]);
+            row += stride;
         }
     }
     if (partial == nullptr) return;
