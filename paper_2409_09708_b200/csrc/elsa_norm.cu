@@ -24,8 +24,8 @@ struct Group {
 };
 
 // CTAs of the gradient kernel on an SM: what its registers allow (two sums and three tensors' vectors of a row for each vector of a
-// lane).  HBM bounds it: 50432 x 768 with a residual 60 us, 5.2 TB/s, 401408 x 128 71 us, 5.7 (one CTA of
-// eight warps whatever the width: 63 and 109).
+// lane).  HBM bounds it: 50432 x 768 with a residual 54 us, 5.8 TB/s, 401408 x 128 71 us, 5.7 (one CTA of
+// eight warps whatever the width, one row on its way: 63 and 109).
 constexpr int backward_per_sm(int row_lanes, int vpl)
 {
     const int warps = vpl == 1 ? 28 : vpl == 2 ? 16 : 8, cta_warps = row_lanes > 128 ? row_lanes / 32 : 4;
@@ -149,7 +149,8 @@ layer_norm_backward_kernel(const uint16_t* dY, const uint16_t* __restrict__ S, c
     const int vecs = dim >> 3;
     const float inv_dim = 1.0f / (float)dim;
     const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-    // rows on their way: two where the registers of a lane hold them
+    // rows on their way: two where it takes eight warps with three vectors a lane to fill the registers (768 columns 60 to 54 us; with one or
+    // two vectors more warps do the same, with four the registers are full)
     constexpr int kAhead = kVpl == 3 && kRowWarps <= 8 ? 2 : 1;
     struct Row {
         uint4 x[kVpl], d[kVpl], r[kAdd ? kVpl : 1];
