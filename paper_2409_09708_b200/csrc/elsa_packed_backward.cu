@@ -46,7 +46,7 @@ struct BackwardShape {
     static constexpr int kTmemCols = 512 / kPerSm;
     static constexpr int kKeptBytes = TileShape<kD>::bytes(128), kWalkBytes = TileShape<kD>::bytes(kWalk);
     static constexpr int kAcc1 = 128 * kGroups, kAcc2 = kAcc1 + kD;  // tensor-memory columns; stage g: S at 128 g, T at 128 g + 64
-    static constexpr int kX1 = kAcc1, kX2 = kAcc1 + kD / 2;          // in the first kernel, which has no acc1
+    enum { kX1 = kAcc1, kX2 = kAcc1 + kD / 2 };                       // X1 and X2 of the first kernel, which has no acc1
     static_assert(kAcc2 + kD <= kTmemCols, "tensor memory");
     static constexpr int kVectorBytes = 2 * kWalk * 4;               // -lse log2(e), -delta
     static constexpr int kSmemBytes = 2 * kKeptBytes + kRing * (2 * kWalkBytes + kVectorBytes) + 1024 /* alignment */ + 256 /* barriers */;
@@ -271,22 +271,17 @@ __global__ void __launch_bounds__(BackwardShape<kD, kKeys, kGroupsOf>::kThreads,
         auto scores = [&](int u, uint32_t y_round) {
             const int g = u % kGroups;
             const uint32_t t_s = tmem_u + (uint32_t)(128 * g), y_at = y1_rows + y_round + (uint32_t)(u * 2) * kY2;
-            if constexpr (!kKeys) {
 #pragma unroll
-                for (int k = 0; k < kD / 16; ++k)
-                    umma_f16_ts_if(t_s, tmem_u + (uint32_t)(B::kX1 + 8 * k), Desc::of(y_at + Desc::k_step(kWalk, k)), p.idesc_s, (uint32_t)(k != 0), elected);
+            for (int x = 0; x < 2; ++x) {
 #pragma unroll
-                for (int k = 0; k < kD / 16; ++k)
-                    umma_f16_ts_if(t_s + 64, tmem_u + (uint32_t)(B::kX2 + 8 * k), Desc::of(y_at + kY2 + Desc::k_step(kWalk, k)), p.idesc_s, (uint32_t)(k != 0), elected);
-                umma_commit_if(bar(kSFull, g), elected);
-                return;
+                for (int k = 0; k < kD / 16; ++k) {
+                    const uint64_t y = Desc::of(y_at + (uint32_t)x * kY2 + Desc::k_step(kWalk, k));
+                    if constexpr (kKeys)
+                        umma_f16_if(t_s + (uint32_t)(64 * x), Desc::of((x == 0 ? x1_desc : x2_desc) + Desc::k_step(128, k)), y, p.idesc_s, (uint32_t)(k != 0), elected);
+                    else
+                        umma_f16_ts_if(t_s + (uint32_t)(64 * x), tmem_u + (uint32_t)((x == 0 ? B::kX1 : B::kX2) + 8 * k), y, p.idesc_s, (uint32_t)(k != 0), elected);
+                }
             }
-#pragma unroll
-            for (int k = 0; k < kD / 16; ++k)
-                umma_f16_if(t_s, Desc::of(x1_desc + Desc::k_step(128, k)), Desc::of(y_at + Desc::k_step(kWalk, k)), p.idesc_s, (uint32_t)(k != 0), elected);
-#pragma unroll
-            for (int k = 0; k < kD / 16; ++k)
-                umma_f16_if(t_s + 64, Desc::of(x2_desc + Desc::k_step(128, k)), Desc::of(y_at + kY2 + Desc::k_step(kWalk, k)), p.idesc_s, (uint32_t)(k != 0), elected);
             umma_commit_if(bar(kSFull, g), elected);
         };
         auto sums = [&](int u, uint32_t y_round, bool first, int steps) {
@@ -435,7 +430,8 @@ __global__ void __launch_bounds__(BackwardShape<kD, kKeys, kGroupsOf>::kThreads,
                     tmem_ld_32x32b_x32(t_lane + (uint32_t)(128 * g + 32 * u), rs);
                     tmem_ld_32x32b_x32(t_lane + (uint32_t)(128 * g + 64 + 32 * u), rt);
                     tmem_wait_ld();
-                    uint32_t wp[16], wd[16];
+                    [[maybe_unused]] uint32_t wp[16];
+                    uint32_t wd[16];
 #pragma unroll
                     for (int i = 0; i < 16; i += 2) {
                         uint64_t l2[2], d2[2];               // -lse log2(e) and -delta of two columns each
