@@ -8,6 +8,8 @@ sums of up to 128 products, exponentials of approximate units, sums of probabili
   ds     E_ds = (h + d) |ds| + p sum |da| E_a + d p (sum |da| |v| + |delta|) + t      delta comes from the rounded a; ds rounded once
   dq, dk h |.| + |scale| sum E_ds |k|  and  |scale| sum E_ds |q|
 """
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -337,6 +339,51 @@ def test_memory_of_a_call_belongs_to_its_stream(lib):
     others = [torch.empty(n, dtype=torch.uint8, device="cuda").fill_(0x7f) for n in sizes for _ in range(4)]       # on the current stream
     torch.cuda.synchronize()
     assert len(others) > 0 and all(torch.equal(u, w) for u, w in zip(ref, got))
+
+
+@pytest.mark.gpu
+def test_empty_sequences_alone(lib):
+    """A batch whose rows all belong to no sequence: everything that a call allocates is zero."""
+    qkv, (q, k, v), da = inputs([70], 2, 2, 64, torch.bfloat16)
+    plan = lib.make_packed_plan([9, 9, 9], 70)
+    a, lse = lib.elsa_packed_attention(q, k, v, plan, 2, want_lse=True)
+    for t in (a, lse) + lib.elsa_packed_attention_backward(da, q, k, v, a, lse, plan, 2):
+        assert (t == 0).all()
+
+
+@pytest.mark.gpu
+def test_two_threads_and_the_default_stream(lib):
+    """Calls from two host threads at once, and with the default stream given while another one is current."""
+    work = []
+    for seed, (lengths, D) in enumerate((([300, 80], 64), ([150, 260], 128))):
+        qkv, (q, k, v), da = inputs(lengths, 2, 1, D, torch.float16, seed=60 + seed)
+        work.append((q, k, v, da, lib.make_packed_plan(offsets_of(lengths))))
+
+    def step(q, k, v, da, plan, stream=None):
+        a, lse = lib.elsa_packed_attention(q, k, v, plan, 2, 1, want_lse=True, stream=stream)
+        return (a, lse) + lib.elsa_packed_attention_backward(da, q, k, v, a, lse, plan, 2, 1, stream=stream)
+
+    alone = [step(*w) for w in work]
+    torch.cuda.synchronize()
+    got = [[], []]
+
+    def many(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(50):
+                got[i].append(step(*work[i]))
+            torch.cuda.current_stream().synchronize()
+
+    threads = [threading.Thread(target=many, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        for i in range(2):
+            got[i].append(step(*work[i], stream=torch.cuda.default_stream()))
+    torch.cuda.synchronize()
+    for x, ys in zip(alone, got):
+        assert len(ys) == 51 and all(torch.equal(u, w) for y in ys for u, w in zip(x, y))
 
 
 @pytest.mark.gpu
