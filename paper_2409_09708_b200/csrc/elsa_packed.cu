@@ -360,9 +360,26 @@ packed_attention_kernel(const __grid_constant__ ForwardParams p)
     }
 }
 
+// Sequence i as the offsets have it now: no rows where they are no offsets.  Read in place, so that what was checked is what is used.
+struct PlanSpan {
+    int begin, len, tiles;               // tiles of 128 rows
+    bool bad;
+};
+__device__ __forceinline__ PlanSpan plan_span(const int32_t* offsets, int i, int rows)
+{
+    int b, e;
+    asm volatile("ld.global.s32 %0, [%1];" : "=r"(b) : "l"(offsets + i));
+    asm volatile("ld.global.s32 %0, [%1];" : "=r"(e) : "l"(offsets + i + 1));
+    const bool bad = b < 0 || e < b || e > rows;
+    const int len = bad ? 0 : e - b;
+    return {b, len, len > 0 ? (len - 1) / 128 + 1 : 0, bad};
+}
+
 // One CTA makes the plan: offsets that are no offsets make an empty one, and dev_status tells.  Sequences go into buckets by their number of
-// 128-row tiles, most first (from 1023 tiles on they share one); where they stand inside a bucket does not matter.
-__global__ void __launch_bounds__(1024) packed_plan_kernel(const int32_t* __restrict__ offsets, int sequences, int rows, int* plan, uint32_t* dev_status)
+// 128-row tiles, most first (from 1023 tiles on they share one); where they stand inside a bucket does not matter.  The offsets are read
+// three times.  A caller keeps them as they are meanwhile; where they change all the same, the plan is worth nothing, but every span is
+// checked as it is read and no entry goes behind the lists.
+__global__ void __launch_bounds__(1024) packed_plan_kernel(const int32_t* offsets, int sequences, int rows, int* plan, uint32_t* dev_status)
 {
     __shared__ int count[2][1024], scan[2][1024];
     pdl_wait_for_predecessors();
@@ -371,17 +388,13 @@ __global__ void __launch_bounds__(1024) packed_plan_kernel(const int32_t* __rest
     count[0][tid] = 0;
     count[1][tid] = 0;
     int bad = 0;
-    for (int i = tid; i < sequences; i += 1024) {
-        const int b = __ldg(offsets + i), e = __ldg(offsets + i + 1);
-        bad |= b < 0 || e < b || e > rows;
-    }
+    for (int i = tid; i < sequences; i += 1024) bad |= plan_span(offsets, i, rows).bad;
     bad = __syncthreads_or(bad);
     auto bucket_of = [](int tiles) { return tiles < 1023 ? tiles : 1023; };
     if (!bad) {
         for (int i = tid; i < sequences; i += 1024) {
-            const int len = __ldg(offsets + i + 1) - __ldg(offsets + i);
-            if (len == 0) continue;
-            const int n = (len - 1) / 128 + 1;
+            const int n = plan_span(offsets, i, rows).tiles;
+            if (n == 0) continue;
             atomicAdd(&count[0][bucket_of(n)], n);
             atomicAdd(&count[1][bucket_of(n)], (n + 1) / 2);
         }
@@ -410,30 +423,33 @@ __global__ void __launch_bounds__(1024) packed_plan_kernel(const int32_t* __rest
     for (int l = 0; l < 2; ++l) count[l][mine] = scan[l][tid] - v[l];
     __syncthreads();
     if (bad) return;
-    int4* list[2] = {reinterpret_cast<int4*>(plan + kPlanHeader), reinterpret_cast<int4*>(plan + kPlanHeader) + plan_capacity(rows, sequences, 128)};
+    const int most[2] = {plan_capacity(rows, sequences, 128), plan_capacity(rows, sequences, 256)};
+    int4* list[2] = {reinterpret_cast<int4*>(plan + kPlanHeader), reinterpret_cast<int4*>(plan + kPlanHeader) + most[0]};
+    auto put = [&](int l, int first, int t, int begin, int len) {
+        const unsigned to = (unsigned)first + (unsigned)t;
+        if (to < (unsigned)most[l]) list[l][to] = make_int4(begin, len, t, 0);
+    };
     for (int base = tid - lane; base < sequences; base += 1024) {
         const int i = base + lane;
-        int begin = 0, len = 0, at[2] = {0, 0};
-        if (i < sequences) {
-            begin = __ldg(offsets + i);
-            len = __ldg(offsets + i + 1) - begin;
-        }
-        const int n = len > 0 ? (len - 1) / 128 + 1 : 0;
+        PlanSpan s = {0, 0, 0, false};
+        if (i < sequences) s = plan_span(offsets, i, rows);
+        const int begin = s.begin, len = s.len, n = s.tiles;
+        int at[2] = {0, 0};
         if (n > 0) {
             at[0] = atomicAdd(&count[0][bucket_of(n)], n);
             at[1] = atomicAdd(&count[1][bucket_of(n)], (n + 1) / 2);
         }
         if (n <= 4) {
-            for (int t = 0; t < n; ++t) list[0][at[0] + t] = make_int4(begin, len, t, 0);
-            for (int t = 0; t < (n + 1) / 2; ++t) list[1][at[1] + t] = make_int4(begin, len, t, 0);
+            for (int t = 0; t < n; ++t) put(0, at[0], t, begin, len);
+            for (int t = 0; t < (n + 1) / 2; ++t) put(1, at[1], t, begin, len);
         }
         // long ones by the whole warp
         for (unsigned todo = __ballot_sync(0xFFFFFFFFu, n > 4); todo != 0; todo &= todo - 1) {
             const int from = __ffs(todo) - 1;
             const int b = __shfl_sync(0xFFFFFFFFu, begin, from), l = __shfl_sync(0xFFFFFFFFu, len, from), m = __shfl_sync(0xFFFFFFFFu, n, from);
             const int a0 = __shfl_sync(0xFFFFFFFFu, at[0], from), a1 = __shfl_sync(0xFFFFFFFFu, at[1], from);
-            for (int t = lane; t < m; t += 32) list[0][a0 + t] = make_int4(b, l, t, 0);
-            for (int t = lane; t < (m + 1) / 2; t += 32) list[1][a1 + t] = make_int4(b, l, t, 0);
+            for (int t = lane; t < m; t += 32) put(0, a0, t, b, l);
+            for (int t = lane; t < (m + 1) / 2; t += 32) put(1, a1, t, b, l);
         }
     }
 }
