@@ -531,9 +531,9 @@ class PackedPlan:
 
 
 def make_packed_plan(offsets, rows=None, device="cuda", dev_status=None, stream=None):
-    """Plan of a batch with sequence i in rows [offsets[i], offsets[i + 1]).  offsets: a list or a CPU tensor, checked here, or an
-    int32 tensor on the device, checked there (dev_status); rows: of the tensors, at least the last offset (default: it).  A
-    captured call reads the plan at every replay: keep it."""
+    """Plan of a batch with sequence i in rows [offsets[i], offsets[i + 1]).  offsets: a list or a CPU tensor, checked here and copied on
+    the plan's stream, which is waited for, or an int32 tensor on the device, checked there (dev_status); rows: of the tensors, at
+    least the last offset (default: it).  A captured call reads the plan at every replay: keep it."""
     full = False
     if rows is not None and not 0 <= rows < 1 << 31:
         raise ValueError("rows=%s does not fit an int" % rows)
@@ -544,13 +544,14 @@ def make_packed_plan(offsets, rows=None, device="cuda", dev_status=None, stream=
         if len(host) < 2 or host[0] < 0 or any(a > b for a, b in zip(host, host[1:])) or host[-1] > rows:
             raise ValueError("offsets must be two or more, not decreasing, within 0 .. rows=%s" % rows)
         full = host[0] == 0 and host[-1] == rows
-        offsets = torch.tensor(host, dtype=torch.int32).to(device)
+        with torch.cuda.stream(stream):                                 # its own memory is used on this stream; None: as it is
+            offsets = torch.tensor(host, dtype=torch.int32).to(device)
     elif offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.numel() < 2 or rows is None:
         raise ValueError("offsets on the device: an int32 vector of two or more, and the number of rows")
     if offsets.get_device() != torch.cuda.current_device():
         raise ValueError("offsets on %s, the current device is cuda:%d" % (offsets.device, torch.cuda.current_device()))
     nbytes = int(_packed_plan_bytes(rows, offsets.numel() - 1))
-    with torch.cuda.stream(stream):                                     # None: as it is
+    with torch.cuda.stream(stream):
         buffer = torch.empty((max(nbytes, 16),), dtype=torch.uint8, device=offsets.device)
     _check(_packed_plan(_ptr(offsets), offsets.numel() - 1, rows, _ptr(buffer), nbytes, _ptr(dev_status), _stream(stream)))
     return PackedPlan(offsets, rows, full, buffer)

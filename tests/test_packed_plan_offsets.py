@@ -35,3 +35,30 @@ def test_offsets_that_change_while_the_plan_is_made(lib):
             lib._check(lib._packed_plan(offsets.data_ptr(), sequences, rows, room.data_ptr(), need, None, lib._stream(None)))
     torch.cuda.synchronize()
     assert (room[need:] == 0x5a).all()
+
+
+@pytest.mark.gpu
+def test_plans_from_lists_on_a_stream_that_is_behind(lib):
+    """Plans made from lists on a busy stream that is not current, each bound to the same name as the one before: every batch keeps
+    its own boundaries, whatever the current stream does with memory that is free."""
+    heads, D, rows = 2, 64, 400
+    qkv = torch.randn((rows, 3 * heads * D), device="cuda", generator=torch.Generator("cuda").manual_seed(1)).half()
+    q, k, v = qkv.split(heads * D, dim=1)
+    batches = [[0, n, rows - n // 2, rows] for n in range(20, 200, 20)]
+    want = [lib.elsa_packed_attention(q, k, v, lib.make_packed_plan(b), heads)[0] for b in batches]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for fill in (False, True):
+        got = []
+        for b in batches:
+            with torch.cuda.stream(side):
+                torch.cuda._sleep(20_000_000)
+            plan = lib.make_packed_plan(b, stream=side)
+            got.append(lib.elsa_packed_attention(q, k, v, plan, heads, stream=side)[0])
+            del plan
+            if fill:
+                others = [torch.full((len(b),), rows // 2, dtype=torch.int32, device="cuda") for _ in range(8)]
+        torch.cuda.synchronize()
+        for x, y in zip(want, got):
+            assert torch.equal(x, y)
+    assert len(others) == 8
