@@ -538,7 +538,10 @@ def make_packed_plan(offsets, rows=None, device="cuda", dev_status=None, stream=
     if rows is not None and not 0 <= rows < 1 << 31:
         raise ValueError("rows=%s does not fit an int" % rows)
     if not torch.is_tensor(offsets) or not offsets.is_cuda:
-        host = [int(o) for o in (offsets.tolist() if torch.is_tensor(offsets) else offsets)]
+        host = offsets.tolist() if torch.is_tensor(offsets) else list(offsets)
+        if any(o % 1 != 0 for o in host):
+            raise ValueError("offsets must be whole numbers")
+        host = [int(o) for o in host]
         if rows is None and host:
             rows = host[-1]
         if len(host) < 2 or host[0] < 0 or any(a > b for a, b in zip(host, host[1:])) or host[-1] > rows:

@@ -10,6 +10,13 @@ def lib():
     return binding
 
 
+def test_offsets_between_two_rows(lib):
+    """Offsets that are no whole numbers are refused, not cut short: no place on the device is asked for."""
+    for bad in ([0, 2.5, 5], torch.tensor([0.0, 2.25, 4.0]), np.array([0.5, 4.0]), [0, float("nan")]):
+        with pytest.raises(ValueError, match="offsets"):
+            lib.make_packed_plan(bad, rows=9)
+
+
 @pytest.mark.gpu
 def test_offsets_that_change_while_the_plan_is_made(lib):
     """A plan from offsets that another stream rewrites meanwhile is worth nothing, but nothing outside it is written.  The two lists
