@@ -535,6 +535,8 @@ def make_packed_plan(offsets, rows=None, device="cuda", dev_status=None, stream=
     the plan's stream, which is waited for, or an int32 tensor on the device, checked there (dev_status); rows: of the tensors, at
     least the last offset (default: it).  A captured call reads the plan at every replay: keep it."""
     full = False
+    if dev_status is not None and not dev_status.is_cuda:
+        raise ValueError("dev_status on %s, CUDA tensor expected" % dev_status.device)
     if rows is not None and not 0 <= rows < 1 << 31:
         raise ValueError("rows=%s does not fit an int" % rows)
     if not torch.is_tensor(offsets) or not offsets.is_cuda:
@@ -551,8 +553,9 @@ def make_packed_plan(offsets, rows=None, device="cuda", dev_status=None, stream=
             offsets = torch.tensor(host, dtype=torch.int32).to(device)
     elif offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.numel() < 2 or rows is None:
         raise ValueError("offsets on the device: an int32 vector of two or more, and the number of rows")
-    if offsets.get_device() != torch.cuda.current_device():
-        raise ValueError("offsets on %s, the current device is cuda:%d" % (offsets.device, torch.cuda.current_device()))
+    for name, t in (("offsets", offsets), ("dev_status", dev_status)):
+        if t is not None and t.get_device() != torch.cuda.current_device():
+            raise ValueError("%s on %s, the current device is cuda:%d" % (name, t.device, torch.cuda.current_device()))
     nbytes = int(_packed_plan_bytes(rows, offsets.numel() - 1))
     with torch.cuda.stream(stream):
         buffer = torch.empty((max(nbytes, 16),), dtype=torch.uint8, device=offsets.device)

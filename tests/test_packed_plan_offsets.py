@@ -17,6 +17,13 @@ def test_offsets_between_two_rows(lib):
             lib.make_packed_plan(bad, rows=9)
 
 
+def test_status_word_that_is_not_on_the_device(lib):
+    """The kernel would write to it where the offsets are none: refused before anything is launched."""
+    for status in (torch.zeros(1, dtype=torch.int32), torch.zeros(1, dtype=torch.int32).expand(4)):
+        with pytest.raises(ValueError, match="dev_status"):
+            lib.make_packed_plan([0, 5], rows=9, dev_status=status)
+
+
 @pytest.mark.gpu
 def test_offsets_that_change_while_the_plan_is_made(lib):
     """A plan from offsets that another stream rewrites meanwhile is worth nothing, but nothing outside it is written.  The two lists
