@@ -363,6 +363,8 @@ __global__ void __launch_bounds__(BackwardShape<kD, kKeys, kGroupsOf>::kThreads,
         const bool exists = row < tile.len;
         const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16);
         float minus_lse = 0.f, minus_delta = 0.f;
+        // all keys of the warp's rows are in the first walked tile (under a causal mask those of the first 64 rows, however long the sequence)
+        [[maybe_unused]] const bool one_tile = (p.causal && row0 + 32 < tile.len ? row0 + 32 : tile.len) <= kWalk;
         if constexpr (!kKeys) {
             // delta, by each group for itself: an exchange would be one more wait, and the rows are in the caches
             RowProducts<kBf16, kD> delta;
@@ -386,7 +388,7 @@ __global__ void __launch_bounds__(BackwardShape<kD, kKeys, kGroupsOf>::kThreads,
                 minus_lse = -1.4426950408889634f * lse;
                 if (g == 0) {
                     p.minus_lse[at] = minus_lse;
-                    if (n > 1) p.minus_delta[at] = minus_delta;
+                    if (!one_tile) p.minus_delta[at] = minus_delta;
                 }
             }
         }
@@ -407,8 +409,9 @@ __global__ void __launch_bounds__(BackwardShape<kD, kKeys, kGroupsOf>::kThreads,
                 const bool whole = __all_sync(0xFFFFFFFFu, lo <= 0 && hi >= kWalk);
                 const uint32_t vec = vectors + (uint32_t)(s * B::kVectorBytes);
                 // With all keys of a row in one tile delta is the sum of p T, exact: from the rounded a it is off by half a step of a, as much as
-                // ds itself where there are few keys (with 64 of them an eighth of that).
-                if (!kKeys && n == 1) {
+                // ds itself where there are few keys (with 64 of them an eighth of that).  The first tile is the first group's, and no later one
+                // has a key for these rows.
+                if (!kKeys && one_tile && it == 0) {
                     float sum = 0.f;
 #pragma unroll 1
                     for (int c = 0; c < kWalk; c += 16) {
