@@ -591,7 +591,8 @@ elsa_status elsa_rotary(const void* x, long long x_pitch, const int32_t* positio
  * q [rows][heads * head_dim], k and v [rows][kv_heads * head_dim]: heads side by side in a row, rows *_pitch values apart
  * (so the thirds of a qkv tensor are taken as they lie); head_dim 32, 64 or 128; pitches multiples of 8.
  * lse (or NULL; needed for the gradient): fp32 [heads][rows], log of the sum of exp(scale * q . k).  Scores, sums and
- * outputs are kept in fp32; the probabilities, and in the gradient ds, are rounded to dtype for the tensor cores.
+ * outputs are kept in fp32; the probabilities, and in the gradient ds, are rounded to dtype for the tensor cores (fp16: with a power
+ * of two on them that keeps them off the ends of its range, for ds by the largest values of da and v in the sequence).
  */
 typedef struct {
     const void* q;
@@ -609,8 +610,8 @@ elsa_status elsa_packed_attention(const elsa_packed_qkv* in, elsa_dtype dtype, c
                                   long long a_pitch, float* lse, uint32_t* dev_status, void* stream);
 /*
  * The gradient, da arriving at a: dq like q, dk and dv like k and v (rows dq_pitch, dk_pitch, dv_pitch values apart, so
- * they may be the thirds of one tensor), sums over the query heads of a key head included.  a and lse: the forward
- * call's.  workspace: elsa_packed_attention_workspace_bytes(rows, heads) bytes, 256-byte aligned.
+ * they may be the thirds of one tensor), sums over the query heads of a key head included (dk and dv may hold other values until
+ * the call has run).  a and lse: the forward call's.  workspace: elsa_packed_attention_workspace_bytes(rows, heads) bytes, 256-byte aligned.
  */
 size_t elsa_packed_attention_workspace_bytes(int rows, int heads);
 elsa_status elsa_packed_attention_backward(const elsa_packed_qkv* in, elsa_dtype dtype, const void* plan, int sequences,

@@ -12,6 +12,10 @@
 //     T  = X2 Y2^T                                               da v^T           v da^T
 //     acc2 += ds Y1  (ds rounded to the 16-bit type)             ds k             ds^T q
 //     acc1 += p Y2   (p rounded to the 16-bit type)              -                p^T da
+// fp16 has too few exponents for them as they are: of 1000 keys and da of 1e-4 ds is 1 % off, of 16384 keys and 1e-5 it is lost, and large
+// ones pass 65504.  So p carries 2^12 there (twelve binary orders more for many keys, four left above 1), and ds the power of two that
+// puts the bound of |da_i . (v_j - a_i)| in the sequence, 2 kD times its largest |da| and |v|, just under 2^15; both leave the sums in fp32 at the
+// end.  The largest values take a pass of their own over da and v (packed_range_kernel).  bf16 has fp32's exponents.
 // All products run on tcgen05; S and T go to fp32 columns of tensor memory, p and ds come back over them as A operands.  A stage of
 // S and T has four warps of its own (a row a lane): one stage's exponentials run under the others' products.
 // The dq kernel has room in tensor memory for X1 and X2 too: a product of 64 columns with A there takes 32 cycles, with A in shared
@@ -58,12 +62,15 @@ struct BackwardParams {
     const int* plan;
     const uint16_t* a;                   // dq kernel: for delta
     const uint16_t* da;
+    const uint16_t* v;                   // for the ranges
     const float* lse;                    // [heads][rows]
     float* minus_lse;                    // [heads][rows]: -lse log2(e), made by the dq kernel for the other
     float* minus_delta;                  // [heads][rows]
-    uint16_t* out1;                      // dv
+    uint16_t* out1;                      // dv; in the dq kernel of fp16 dk, for the key tiles' factors
     uint16_t* out2;                      // dq or dk
-    long long a_pitch, da_pitch, out1_pitch, out2_pitch;
+    const uint16_t* range;               // dq kernel of fp16: dv, where the tiles' ranges stand
+    long long range_pitch;
+    long long a_pitch, da_pitch, v_pitch, out1_pitch, out2_pitch;
     int rows, sequences, heads, kv_heads, group;
     int causal;
     float scale, scale_log2;
@@ -156,6 +163,94 @@ struct RowProducts {
     }
 };
 
+constexpr int kPBits = 12;               // fp16: p carries 2^12 in the dk, dv kernel
+
+// The ranges of fp16 stand in rows of the outputs that the dk, dv kernel has yet to write (the workspace has no room for them): of a tile of 128 rows
+// and key head the largest |da| and |v|, a word of two fp16, in dv at the tile's first row; the dq kernel makes the factor of a sequence from
+// them and leaves it for the dk, dv kernel in dk at the first row of each tile, which only that tile's own CTA reads, before it writes there.
+__device__ __forceinline__ long long range_at(long long pitch, const PackedTile& t, int tile, int kv_head, int head_dim)
+{
+    return (long long)(t.begin + 128 * tile) * pitch + (long long)kv_head * head_dim;
+}
+
+// Binary orders that ds carries: 2 kD |da| |v| times 2^that is in [2^14, 2^15), none where it is zero.  The largest values are finite: no overflow.
+template <int kD>
+__device__ __forceinline__ int ds_orders(uint32_t da_bits, uint32_t v_bits)
+{
+    const float most = (float)(2 * kD) * (__half2float(__ushort_as_half((unsigned short)da_bits)) * __half2float(__ushort_as_half((unsigned short)v_bits)));
+    return most > 0.f ? 15 - ((int)(__float_as_uint(most) >> 23) - 126) : 0;
+}
+// 2^n, n far inside fp32's exponents.
+__device__ __forceinline__ float power_of_two(int n) { return __uint_as_float((uint32_t)(n + 127) << 23); }
+
+// A CTA per tile of 128 rows and key head: the largest |v|, and the largest |da| of the query heads that share it.  Infinities and NaN do not
+// count: what they reach has no finite value, the rest keeps its own.  HBM bounds it, da and v are read once: 21 us for 64 images of 49 to 1024
+// rows, 12 heads of 64, whose gradient takes 442 with it and 412 in bf16; a launch of 2.3 us for 8 small ones (17.0 and 14.7).  Largest norms of rows
+// instead of largest values are a bound three to four orders nearer, 25 us, and more than the orders are worth.
+constexpr int kRangeThreads = 256;
+struct RangeParams {
+    const int* plan;
+    const uint16_t *da, *v;
+    uint16_t* dv;
+    long long da_pitch, v_pitch, dv_pitch;
+    int rows, sequences, kv_heads, group;
+    uint32_t* dev_status;
+};
+template <int kD>
+__global__ void __launch_bounds__(kRangeThreads) packed_range_kernel(const RangeParams p)
+{
+    constexpr int kLanes = kD / 8, kRows = kRangeThreads / kLanes, kSteps = 128 / kRows;
+    __shared__ uint32_t tops[kRangeThreads / 32];
+    pdl_wait_for_predecessors();
+    pdl_release_successors();
+    PackedTile tile;
+    const int kv_head = blockIdx.x % p.kv_heads, index = blockIdx.x / p.kv_heads;
+    const int4 entry = plan_entry<128>(p.plan, p.rows, p.sequences, index);
+    if (index >= plan_tiles<128>(p.plan, p.rows, p.sequences, p.dev_status) || !plan_tile<128>(entry, p.rows, false, tile)) return;
+    const int row0 = threadIdx.x / kLanes, sub = threadIdx.x % kLanes;
+    struct Rows {
+        uint4 u[kSteps];
+    };
+    auto load = [&](Rows& r, const uint16_t* x, long long pitch, int head) {
+        x += (long long)(tile.begin + tile.first + row0) * pitch + (long long)head * kD + 8 * sub;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i)
+            r.u[i] = tile.first + row0 + kRows * i < tile.len ? __ldg(reinterpret_cast<const uint4*>(x + (long long)(kRows * i) * pitch)) : make_uint4(0u, 0u, 0u, 0u);
+    };
+    // |x| of two values as 16-bit integers in order, 0x400 higher: what is not finite is below zero
+    uint32_t top_v = 0u, top_da = 0u;
+    auto add = [&](const Rows& r, uint32_t& top) {
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            top = __vmaxs2(top, (r.u[i].x & 0x7fff7fffu) + 0x04000400u);
+            top = __vmaxs2(top, (r.u[i].y & 0x7fff7fffu) + 0x04000400u);
+            top = __vmaxs2(top, (r.u[i].z & 0x7fff7fffu) + 0x04000400u);
+            top = __vmaxs2(top, (r.u[i].w & 0x7fff7fffu) + 0x04000400u);
+        }
+    };
+    Rows v, da;
+    load(v, p.v, p.v_pitch, kv_head);
+    load(da, p.da, p.da_pitch, kv_head * p.group);
+    add(v, top_v);
+    for (int h = 1; h < p.group; ++h) {
+        const Rows had = da;
+        load(da, p.da, p.da_pitch, kv_head * p.group + h);         // on its way while the head before is looked through
+        add(had, top_da);
+    }
+    add(da, top_da);
+    auto warp_top = [](uint32_t t) { return __reduce_max_sync(0xFFFFFFFFu, max(t & 0xffffu, t >> 16)); };
+    const uint32_t both = warp_top(top_da) << 16 | warp_top(top_v);
+    if (threadIdx.x % 32 == 0) tops[threadIdx.x / 32] = both;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        const uint32_t t = tops[threadIdx.x % (kRangeThreads / 32)];
+        const uint32_t da_bits = __reduce_max_sync(0xFFFFFFFFu, t >> 16), v_bits = __reduce_max_sync(0xFFFFFFFFu, t & 0xffffu);
+        auto bits = [](uint32_t t) { return t > 0x400u ? t - 0x400u : 0u; };
+        if (threadIdx.x == 0)
+            *reinterpret_cast<uint32_t*>(p.dv + range_at(p.dv_pitch, tile, tile.first / 128, kv_head, kD)) = bits(da_bits) << 16 | bits(v_bits);
+    }
+}
+
 template <bool kBf16, int kD, bool kKeys, int kGroupsOf>
 __global__ void __launch_bounds__(BackwardShape<kD, kKeys, kGroupsOf>::kThreads, BackwardShape<kD, kKeys, kGroupsOf>::kPerSm) packed_attention_backward_kernel(const __grid_constant__ BackwardParams p)
 {
@@ -209,6 +304,18 @@ __global__ void __launch_bounds__(BackwardShape<kD, kKeys, kGroupsOf>::kThreads,
         }
         __syncwarp();
         tmem_alloc(tmem_holder_addr, B::kTmemCols);
+    }
+    [[maybe_unused]] int orders = 0;                                 // that ds carries, 2^orders times its value
+    [[maybe_unused]] uint32_t range = 0u;
+    if constexpr (!kBf16) {
+        if (warp < kTmaWarp) {
+            if constexpr (kKeys) {
+                // ahead of the barrier: one of the warps writes there at the end
+                asm volatile("ld.global.cg.s32 %0, [%1];" : "=r"(orders) : "l"(p.out2 + range_at(p.out2_pitch, tile, tile.first / 128, head, kD)) : "memory");
+            } else if (lane <= (tile.len - 1) / 128) {
+                asm volatile("ld.global.cg.u32 %0, [%1];" : "=r"(range) : "l"(p.range + range_at(p.range_pitch, tile, lane, head / p.group, kD)));
+            }
+        }
     }
     tc_fence_before();
     __syncthreads();
@@ -362,6 +469,8 @@ __global__ void __launch_bounds__(BackwardShape<kD, kKeys, kGroupsOf>::kThreads,
         const int row0 = tile.first + 32 * quarter, row = row0 + lane;                 // kept row, in the sequence
         const bool exists = row < tile.len;
         const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16);
+        // delta as the dk, dv kernel of fp16 takes it, ds's power of two less the one that is in p there
+        auto handed_delta = [&](float d) { return kBf16 ? d : d * power_of_two(orders - kPBits); };
         float minus_lse = 0.f, minus_delta = 0.f;
         // all keys of the warp's rows are in the first walked tile (under a causal mask those of the first 64 rows, however long the sequence)
         [[maybe_unused]] const bool one_tile = (p.causal && row0 + 32 < tile.len ? row0 + 32 : tile.len) <= kWalk;
@@ -383,16 +492,29 @@ __global__ void __launch_bounds__(BackwardShape<kD, kKeys, kGroupsOf>::kThreads,
                 if (lane == 0) mbar_arrive(bar(kXMoved, 0));
             }
             minus_delta = -delta.sums();
+            if constexpr (!kBf16) {
+                for (int t = lane + 32; t <= (tile.len - 1) / 128; t += 32) {
+                    uint32_t more;
+                    asm volatile("ld.global.cg.u32 %0, [%1];" : "=r"(more) : "l"(p.range + range_at(p.range_pitch, tile, t, head / p.group, kD)));
+                    range = __vmaxu2(range, more);
+                }
+                orders = ds_orders<kD>(__reduce_max_sync(0xFFFFFFFFu, range >> 16), __reduce_max_sync(0xFFFFFFFFu, range & 0xffffu));
+                if (warp == 0 && lane == 0 && head % p.group == 0)
+                    *reinterpret_cast<int*>(p.out1 + range_at(p.out1_pitch, tile, tile.first / 128, head / p.group, kD)) = orders;
+            }
             if (exists) {
                 const size_t at = (size_t)head * (size_t)p.rows + (size_t)(tile.begin + row);
                 minus_lse = -1.4426950408889634f * lse;
                 if (g == 0) {
-                    p.minus_lse[at] = minus_lse;
-                    if (!one_tile) p.minus_delta[at] = minus_delta;
+                    p.minus_lse[at] = kBf16 ? minus_lse : minus_lse + (float)kPBits;
+                    if (!one_tile) p.minus_delta[at] = handed_delta(minus_delta);
                 }
             }
         }
         const uint64_t scale2 = f32x2(p.scale_log2, p.scale_log2);
+        // fp16: the dq kernel has the power of two for ds in the exponential, the other in T and delta, since its p goes to dv
+        [[maybe_unused]] const float minus_lse_ds = kBf16 ? minus_lse : minus_lse + (float)orders;
+        [[maybe_unused]] const uint64_t t_factor2 = f32x2(power_of_two(orders - kPBits), power_of_two(orders - kPBits));
         for (int it = g; it < n; it += kGroups) {
             const int s = it % kRing;
             const int walked = (walk_from + it % per_head) * kWalk;                    // first walked row, in the sequence
@@ -426,7 +548,7 @@ __global__ void __launch_bounds__(BackwardShape<kD, kKeys, kGroupsOf>::kThreads,
                         }
                     }
                     minus_delta = -sum;
-                    if (exists) p.minus_delta[(size_t)head * (size_t)p.rows + (size_t)(tile.begin + row)] = minus_delta;
+                    if (exists) p.minus_delta[(size_t)head * (size_t)p.rows + (size_t)(tile.begin + row)] = handed_delta(minus_delta);
                 }
                 auto unit = [&](auto masked, int u) {
                     uint32_t rs[32], rt[32];
@@ -442,7 +564,7 @@ __global__ void __launch_bounds__(BackwardShape<kD, kKeys, kGroupsOf>::kThreads,
                             asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(l2[0]), "=l"(l2[1]) : "r"(vec + (uint32_t)(128 * u + 8 * i)));
                             asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(d2[0]), "=l"(d2[1]) : "r"(vec + (uint32_t)(4 * kWalk + 128 * u + 8 * i)));
                         } else {
-                            l2[0] = l2[1] = f32x2(minus_lse, minus_lse);
+                            l2[0] = l2[1] = f32x2(minus_lse_ds, minus_lse_ds);
                             d2[0] = d2[1] = f32x2(minus_delta, minus_delta);
                         }
 #pragma unroll
@@ -450,7 +572,8 @@ __global__ void __launch_bounds__(BackwardShape<kD, kKeys, kGroupsOf>::kThreads,
                             const int c = 2 * (i + h), col = 32 * u + c;
                             const float2 e = f32x2_split(f32x2_fma(f32x2(__uint_as_float(rs[c]), __uint_as_float(rs[c + 1])), scale2, l2[h]));
                             float2 pp = make_float2(exp2_approx(e.x), exp2_approx(e.y));
-                            float2 ds = f32x2_split(f32x2_mul(f32x2(pp.x, pp.y), f32x2_add(f32x2(__uint_as_float(rt[c]), __uint_as_float(rt[c + 1])), d2[h])));
+                            const uint64_t t2 = f32x2(__uint_as_float(rt[c]), __uint_as_float(rt[c + 1]));
+                            float2 ds = f32x2_split(f32x2_mul(f32x2(pp.x, pp.y), kBf16 || !kKeys ? f32x2_add(t2, d2[h]) : f32x2_fma(t2, t_factor2, d2[h])));
                             if constexpr (decltype(masked)::value) {
                                 if (col < lo || col >= hi) pp.x = ds.x = 0.f;
                                 if (col + 1 < lo || col + 1 >= hi) pp.y = ds.y = 0.f;
@@ -491,6 +614,7 @@ __global__ void __launch_bounds__(BackwardShape<kD, kKeys, kGroupsOf>::kThreads,
             // all copies and products have ended: the ring is staging room
             const uint32_t stage = y1_smem(0) + (uint32_t)(32 * 2 * TileShape<kD>::kCols * warp);
             const long long first = tile.begin + row0;
+            const float ds_scale = kBf16 ? p.scale : p.scale * power_of_two(-orders);
             if constexpr (kKeys) {
                 constexpr int kCols = TileShape<kD>::kCols;
 #pragma unroll
@@ -499,14 +623,14 @@ __global__ void __launch_bounds__(BackwardShape<kD, kKeys, kGroupsOf>::kThreads,
                     uint16_t* dst = (o == 0 ? p.out1 + first * p.out1_pitch : p.out2 + first * p.out2_pitch) + head * kD;
 #pragma unroll
                     for (int c = 0; c < kD; c += kCols)
-                        store_rows<kBf16, kCols>(t_lane + (uint32_t)((o == 0 ? B::kAcc1 : B::kAcc2) + c), o == 0 ? 1.f : p.scale, stage, dst + c,
+                        store_rows<kBf16, kCols>(t_lane + (uint32_t)((o == 0 ? B::kAcc1 : B::kAcc2) + c), o == 0 ? (kBf16 ? 1.f : power_of_two(-kPBits)) : ds_scale, stage, dst + c,
                                                  o == 0 ? p.out1_pitch : p.out2_pitch, tile.len - row0, lane);
                 }
             } else {
                 // the columns, in halves by the first two groups where there are more than one and each half has 32
                 constexpr int kCols = kGroups > 1 && kD > 32 ? kD / 2 : kD;
                 if (kCols * g < kD)
-                    store_rows<kBf16, kCols>(t_lane + (uint32_t)(B::kAcc2 + kCols * g), p.scale, stage, p.out2 + first * p.out2_pitch + head * kD + kCols * g,
+                    store_rows<kBf16, kCols>(t_lane + (uint32_t)(B::kAcc2 + kCols * g), ds_scale, stage, p.out2 + first * p.out2_pitch + head * kD + kCols * g,
                                              p.out2_pitch, tile.len - row0, lane);
             }
         }
@@ -543,10 +667,29 @@ elsa_status launch(const BackwardParams& p, cudaStream_t stream, const DeviceInf
     return launched("packed_attention_backward");
 }
 
+template <int kD>
+elsa_status launch_range(const BackwardParams& queries, const BackwardParams& keys, cudaStream_t stream)
+{
+    RangeParams r;
+    r.plan = queries.plan; r.da = queries.da; r.v = queries.v; r.dv = keys.out1;
+    r.da_pitch = queries.da_pitch; r.v_pitch = queries.v_pitch; r.dv_pitch = keys.out1_pitch;
+    r.rows = queries.rows; r.sequences = queries.sequences; r.kv_heads = queries.kv_heads; r.group = queries.group;
+    r.dev_status = queries.dev_status;
+    const long long items = (long long)plan_capacity(r.rows, r.sequences, 128) * r.kv_heads;
+    if (items > 0x7fffffffLL) return fail(ELSA_ERR_SHAPE, "tiles * heads does not fit an int");
+    ProfileScope scope(ELSA_KERNEL_PACKED_ATTENTION_BACKWARD, stream);
+    cudaError_t e = launch_pdl(packed_range_kernel<kD>, dim3((unsigned)items), dim3(kRangeThreads), 0, stream, 1, r);
+    if (e != cudaSuccess) return fail(ELSA_ERR_CUDA, "packed range launch: %s", cudaGetErrorString(e));
+    return launched("packed_range");
+}
+
 template <bool kBf16, int kD>
 elsa_status launch_both(const BackwardParams& queries, const BackwardParams& keys, cudaStream_t stream, const DeviceInfo& dev)
 {
     elsa_status st;
+    if constexpr (!kBf16) {
+        if ((st = launch_range<kD>(queries, keys, stream)) != ELSA_OK) return st;
+    }
     if constexpr (kD > 64) {
         st = launch<kBf16, kD, false, 2>(queries, stream, dev);
         return st != ELSA_OK ? st : launch<kBf16, kD, true, 2>(keys, stream, dev);
@@ -574,6 +717,8 @@ elsa_status launch_packed_attention_backward(const elsa_packed_qkv& in, elsa_dty
     const long long wide = (long long)in.heads * d, narrow = (long long)in.kv_heads * d;
     BackwardParams q, k;
     q.plan = plan; q.a = a; q.da = da; q.lse = lse;
+    q.v = static_cast<const uint16_t*>(in.v); q.v_pitch = in.v_pitch;
+    q.range = dv; q.range_pitch = dv_pitch;
     q.minus_lse = static_cast<float*>(workspace);
     q.minus_delta = reinterpret_cast<float*>(static_cast<char*>(workspace) + packed_attention_workspace(rows, in.heads) / 2);
     q.a_pitch = a_pitch; q.da_pitch = da_pitch;
@@ -584,7 +729,7 @@ elsa_status launch_packed_attention_backward(const elsa_packed_qkv& in, elsa_dty
     q.idesc_acc = packed_idesc(dtype, d, true);
     q.dev_status = dev_status;
     k = q;
-    q.out1 = nullptr; q.out1_pitch = 0;
+    q.out1 = dk; q.out1_pitch = dk_pitch;
     q.out2 = dq; q.out2_pitch = dq_pitch;
     k.out1 = dv; k.out1_pitch = dv_pitch;
     k.out2 = dk; k.out2_pitch = dk_pitch;
