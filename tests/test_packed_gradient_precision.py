@@ -190,3 +190,44 @@ def test_a_sequence_keeps_its_own_range(lib, filler, D):
     _, got = both_ways(lib, q, k, v, da, lengths, heads, kv_heads)
     for name in alone:
         assert torch.isfinite(alone[name]).all() and torch.equal(alone[name], got[name][r]), name
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES)
+@pytest.mark.parametrize("causal", [False, True], ids=["full", "causal"])
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_gradient_against_differences_along_itself(lib, D, causal, dtype):
+    """Differences of f = sum of da a, a by the definition in 64 bits, which no formula of the gradient enters, along the kernel's own
+    gradient g: the slope is |g|^2 where g is right.  With g off by a relative e in the Frobenius norm they are e |g|^2 apart at most;
+    e is 8 h: the four roundings of the small-gradients test, twice, since of few keys they do not average out.  A gradient that is
+    zero, has another sign, scale or mask fails.  The third difference leaves step^2, 1e-8, of it."""
+    lengths, heads, kv_heads = [90, 41, 140], 4, 2
+    h, rows, scale = torch.finfo(dtype).eps / 2, sum(lengths), D ** -0.5
+    q, k, v = (synth.randn((rows, w * D), 110 + i, 1.0, dtype, "cuda") for i, w in enumerate((heads, kv_heads, kv_heads)))
+    da = synth.randn((rows, heads * D), 113, 0.5, dtype, "cuda")
+    _, got = both_ways(lib, q, k, v, da, lengths, heads, kv_heads, causal=causal)
+
+    def f(q, k, v):
+        total, starts = 0.0, [0] + np.cumsum(lengths).tolist()
+        for b, e in zip(starts, starts[1:]):
+            for i in range(heads):
+                j = i // (heads // kv_heads)
+                ci, cj = slice(i * D, (i + 1) * D), slice(j * D, (j + 1) * D)
+                s = scale * q[b:e, ci] @ k[b:e, cj].t()
+                if causal:
+                    s = torch.where(torch.ones_like(s, dtype=torch.bool).tril(), s, -torch.inf)
+                total += float(((torch.softmax(s, dim=1) @ v[b:e, cj]) * da[b:e, ci].double()).sum())
+        return total
+
+    for which, name in enumerate(("dq", "dk", "dv")):
+        x, g = [t.double() for t in (q, k, v)], got[name].double()
+        size = float(g.square().sum())
+        step = 1e-4 / size ** 0.5 * x[which].numel() ** 0.5                       # 1e-4 of each value's size on average
+
+        def at(e):
+            y = list(x)
+            y[which] = y[which] + e * g
+            return f(*y)
+
+        slope = (at(step) - at(-step)) / (2 * step)
+        assert size > 1.0 and abs(slope - size) <= (8 * h + 1e-5) * size, "%s: slope %g, %g expected" % (name, slope, size)
