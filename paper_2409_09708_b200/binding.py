@@ -530,11 +530,12 @@ class PackedPlan:
         self.sequences = offsets.numel() - 1
 
 
-def make_packed_plan(offsets, rows=None, device="cuda", dev_status=None, stream=None):
+def make_packed_plan(offsets, rows=None, device="cuda", dev_status=None, stream=None, full=False):
     """Plan of a batch with sequence i in rows [offsets[i], offsets[i + 1]).  offsets: a list or a CPU tensor, checked here and copied on
     the plan's stream, which is waited for, or an int32 tensor on the device, checked there (dev_status); rows: of the tensors, at
-    least the last offset (default: it).  A captured call reads the plan at every replay: keep it."""
-    full = False
+    least the last offset (default: it).  A captured call reads the plan at every replay: keep it.  full: every row belongs to a sequence
+    (see PackedPlan); of a list it is known, offsets on the device are looked at for it, which waits for the plan's stream."""
+    covered = False                                                     # every row, as far as is known
     if dev_status is not None and not dev_status.is_cuda:
         raise ValueError("dev_status on %s, CUDA tensor expected" % dev_status.device)
     if rows is not None and not 0 <= rows < 1 << 31:
@@ -548,7 +549,9 @@ def make_packed_plan(offsets, rows=None, device="cuda", dev_status=None, stream=
             rows = host[-1]
         if len(host) < 2 or host[0] < 0 or any(a > b for a, b in zip(host, host[1:])) or host[-1] > rows:
             raise ValueError("offsets must be two or more, not decreasing, within 0 .. rows=%s" % rows)
-        full = host[0] == 0 and host[-1] == rows
+        covered = host[0] == 0 and host[-1] == rows
+        if full and not covered:
+            raise ValueError("offsets do not cover every row of %d" % rows)
         with torch.cuda.stream(stream):                                 # its own memory is used on this stream; None: as it is
             offsets = torch.tensor(host, dtype=torch.int32).to(device)
     elif offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.numel() < 2 or rows is None:
@@ -556,11 +559,16 @@ def make_packed_plan(offsets, rows=None, device="cuda", dev_status=None, stream=
     for name, t in (("offsets", offsets), ("dev_status", dev_status)):
         if t is not None and t.get_device() != torch.cuda.current_device():
             raise ValueError("%s on %s, the current device is cuda:%d" % (name, t.device, torch.cuda.current_device()))
+    if full and not covered:
+        with torch.cuda.stream(stream):
+            covered = bool((offsets[0] == 0) & (offsets[-1] == rows) & (offsets[1:] >= offsets[:-1]).all())
+    if full and not covered:
+        raise ValueError("offsets do not cover every row of %d" % rows)
     nbytes = int(_packed_plan_bytes(rows, offsets.numel() - 1))
     with torch.cuda.stream(stream):
         buffer = torch.empty((max(nbytes, 16),), dtype=torch.uint8, device=offsets.device)
     _check(_packed_plan(_ptr(offsets), offsets.numel() - 1, rows, _ptr(buffer), nbytes, _ptr(dev_status), _stream(stream)))
-    return PackedPlan(offsets, rows, full, buffer)
+    return PackedPlan(offsets, rows, covered, buffer)
 
 
 def elsa_packed_attention(q, k, v, plan, heads, kv_heads=None, causal=False, scale=None, a=None, want_lse=False, lse=None, dev_status=None,

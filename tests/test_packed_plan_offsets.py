@@ -24,6 +24,29 @@ def test_status_word_that_is_not_on_the_device(lib):
             lib.make_packed_plan([0, 5], rows=9, dev_status=status)
 
 
+def test_a_list_that_leaves_rows_out(lib):
+    for bad, rows in (([1, 5], 5), ([0, 4], 5)):
+        with pytest.raises(ValueError, match="every row"):
+            lib.make_packed_plan(bad, rows, full=True)
+
+
+@pytest.mark.gpu
+def test_full_offsets_on_the_device(lib):
+    """Said to cover every row they are looked at, and outputs are not zeroed; left unsaid, rows of no sequence hold zeros."""
+    qkv = torch.randn((300, 3 * 128), device="cuda", generator=torch.Generator("cuda").manual_seed(2)).half()
+    q, k, v = qkv.split(128, dim=1)
+    def on_device(*o):
+        return torch.tensor(o, dtype=torch.int32, device="cuda")
+    assert lib.make_packed_plan([0, 120, 300]).full and lib.make_packed_plan([0, 120, 300], full=True).full
+    assert not lib.make_packed_plan(on_device(0, 120, 300), 300).full
+    plan = lib.make_packed_plan(on_device(0, 120, 300), 300, full=True)
+    assert plan.full
+    assert torch.equal(lib.elsa_packed_attention(q, k, v, plan, 2)[0], lib.elsa_packed_attention(q, k, v, lib.make_packed_plan([0, 120, 300]), 2)[0])
+    for bad in (on_device(0, 120, 299), on_device(1, 120, 300), on_device(0, 200, 100, 300), on_device(0, 301, 300)):
+        with pytest.raises(ValueError, match="every row"):
+            lib.make_packed_plan(bad, 300, full=True)
+
+
 @pytest.mark.gpu
 def test_offsets_that_change_while_the_plan_is_made(lib):
     """A plan from offsets that another stream rewrites meanwhile is worth nothing, but nothing outside it is written.  The two lists
