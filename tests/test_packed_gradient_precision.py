@@ -231,3 +231,35 @@ def test_gradient_against_differences_along_itself(lib, D, causal, dtype):
 
         slope = (at(step) - at(-step)) / (2 * step)
         assert size > 1.0 and abs(slope - size) <= (8 * h + 1e-5) * size, "%s: slope %g, %g expected" % (name, slope, size)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_captured_with_other_gradients(lib, D):
+    """fp16: a captured gradient into thirds of one tensor takes the range of the da that it finds at each replay, and leaves rows of no
+    sequence alone."""
+    lengths, heads, kv_heads, rows = [130, 1, 300], 4, 2, 450
+    parts = [heads * D, kv_heads * D, kv_heads * D]
+    q, k, v = synth.randn((rows, sum(parts)), 130, 1.0, torch.float16, "cuda").split(parts, dim=1)
+    da = torch.zeros(rows, heads * D, dtype=torch.float16, device="cuda")
+    plan = lib.make_packed_plan([7] + (7 + np.cumsum(lengths)).tolist(), rows)
+    a, lse = lib.elsa_packed_attention(q, k, v, plan, heads, kv_heads, causal=True, want_lse=True)
+    dqkv = torch.full((rows, sum(parts)), 7.0, dtype=torch.float16, device="cuda")
+    dq, dk, dv = dqkv.split(parts, dim=1)
+    work = torch.empty(int(lib._packed_ws(rows, heads)), dtype=torch.uint8, device="cuda")
+    step = lambda: lib.elsa_packed_attention_backward(da, q, k, v, a, lse, plan, heads, kv_heads, causal=True, dq=dq, dk=dk, dv=dv, workspace=work)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for size in (1.0, 1e-5, 300.0, 0.0, 1e-3):
+        da.copy_(synth.randn((rows, heads * D), 131, size, torch.float16, "cuda") if size > 0 else torch.zeros_like(da))
+        dqkv[7:7 + sum(lengths)] = float("nan")
+        graph.replay()
+        torch.cuda.synchronize()
+        got = dqkv.clone()
+        assert torch.isfinite(got).all() and (got[:7] == 7.0).all() and (got[7 + sum(lengths):] == 7.0).all()
+        want = lib.elsa_packed_attention_backward(da, q, k, v, a, lse, plan, heads, kv_heads, causal=True)
+        for x, y in zip(got.split(parts, dim=1), want):
+            assert torch.equal(x[7:7 + sum(lengths)], y[7:7 + sum(lengths)]) and (size > 0 or not y.any())
