@@ -579,7 +579,8 @@ elsa_status elsa_rotary(const void* x, long long x_pitch, const int32_t* positio
  * sequences are allowed; rows before the first and behind the last belong to none).
  *     a[r, h] = sum over j of p_j v[j, h / group],   p = softmax over j of scale * q[r, h] . k[j, h / group]
  * over the rows j of r's own sequence, causal: those up to r; group = heads / kv_heads query heads share a key head.
- * Rows of no sequence are neither read nor written.  Non-finite values of one sequence reach no other; inside a sequence
+ * Rows of no sequence are not written, and may be read (a tile's loads pass the sequence's end), but change no result, whatever
+ * they hold.  Non-finite values of one sequence reach no other; inside a sequence
  * one in v, or in the gradient one in any input, may reach every row of it, a causal mask or not.  Outputs may not overlap
  * inputs.
  *
