@@ -263,38 +263,38 @@ layer_norm_backward_kernel(const uint16_t* dY, const uint16_t* __restrict__ S, c
         }
         return;
     } else {
-    // the row groups of the CTA, one after another in a fixed order: columns [2][dim]
+        // the row groups of the CTA, one after another in a fixed order: columns [2][dim]
 #pragma unroll 1
-    for (int k = 0; k < G::kGroups; ++k) {
-        if (group == k) {
+        for (int k = 0; k < G::kGroups; ++k) {
+            if (group == k) {
 #pragma unroll
-            for (int c = 0; c < kVpl; ++c) {
-                const int v = sub + G::kRowLanes * c;
-                if (v >= vecs) continue;
-                float4* a = reinterpret_cast<float4*>(columns + 8 * v);
-                float4* b = reinterpret_cast<float4*>(columns + dim + 8 * v);
+                for (int c = 0; c < kVpl; ++c) {
+                    const int v = sub + G::kRowLanes * c;
+                    if (v >= vecs) continue;
+                    float4* a = reinterpret_cast<float4*>(columns + 8 * v);
+                    float4* b = reinterpret_cast<float4*>(columns + dim + 8 * v);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float4 p = make_float4(dgain[c][4 * h], dgain[c][4 * h + 1], dgain[c][4 * h + 2], dgain[c][4 * h + 3]);
-                    float4 q = make_float4(dbias[c][4 * h], dbias[c][4 * h + 1], dbias[c][4 * h + 2], dbias[c][4 * h + 3]);
-                    if (k > 0) {
-                        const float4 p0 = a[h], q0 = b[h];
-                        p.x += p0.x; p.y += p0.y; p.z += p0.z; p.w += p0.w;
-                        q.x += q0.x; q.y += q0.y; q.z += q0.z; q.w += q0.w;
-                    }
-                    if (k + 1 < G::kGroups) {
-                        a[h] = p;
-                        b[h] = q;
-                    } else {
-                        float4* out = reinterpret_cast<float4*>(partial + (size_t)blockIdx.x * (size_t)(2 * dim));
-                        out[2 * v + h] = p;
-                        out[(dim >> 2) + 2 * v + h] = q;
+                    for (int h = 0; h < 2; ++h) {
+                        float4 p = make_float4(dgain[c][4 * h], dgain[c][4 * h + 1], dgain[c][4 * h + 2], dgain[c][4 * h + 3]);
+                        float4 q = make_float4(dbias[c][4 * h], dbias[c][4 * h + 1], dbias[c][4 * h + 2], dbias[c][4 * h + 3]);
+                        if (k > 0) {
+                            const float4 p0 = a[h], q0 = b[h];
+                            p.x += p0.x; p.y += p0.y; p.z += p0.z; p.w += p0.w;
+                            q.x += q0.x; q.y += q0.y; q.z += q0.z; q.w += q0.w;
+                        }
+                        if (k + 1 < G::kGroups) {
+                            a[h] = p;
+                            b[h] = q;
+                        } else {
+                            float4* out = reinterpret_cast<float4*>(partial + (size_t)blockIdx.x * (size_t)(2 * dim));
+                            out[2 * v + h] = p;
+                            out[(dim >> 2) + 2 * v + h] = q;
+                        }
                     }
                 }
             }
+            if (G::kGroups > 1) __syncthreads();
         }
-        if (G::kGroups > 1) __syncthreads();
-    }
     }
 }
 
@@ -347,7 +347,8 @@ RowShape row_shape(int dim)
     return best;
 }
 
-// Rows of partial sums: one of each CTA that the 148 SMs of the device hold.
+// Rows of partial sums: one of each CTA that the 148 SMs of sm_100a hold.  A constant, so that a workspace's size is the same wherever it is
+// asked for.
 int max_parts(int dim)
 {
     const RowShape shape = row_shape(dim);
@@ -393,8 +394,7 @@ cudaError_t forward(const RowShape& shape, const uint16_t* A, const uint16_t* R,
 
 template <bool kBf16, bool kAdd>
 cudaError_t backward(const RowShape& shape, const uint16_t* dY, const uint16_t* S, const float2* stats, const uint16_t* gain,
-                     const uint16_t* dS, uint16_t* dX, float* partial, int rows, int dim, int* parts, cudaStream_t stream,
-                     const DeviceInfo& dev)
+                     const uint16_t* dS, uint16_t* dX, float* partial, int rows, int dim, int* parts, cudaStream_t stream)
 {
     cudaError_t e = cudaSuccess;
 #define ELSA_NORM_BACKWARD(LANES, WARPS, VPL)                                                                                  \
@@ -402,7 +402,7 @@ cudaError_t backward(const RowShape& shape, const uint16_t* dY, const uint16_t* 
         using G = Group<LANES, WARPS, 128>;                                                                                    \
         auto kernel = layer_norm_backward_kernel<kBf16, kAdd, LANES, WARPS, VPL>;                                              \
         constexpr bool kShared = WARPS > 8;                                                                                    \
-        const size_t smem = partial != nullptr && (G::kGroups > 1 || kShared) ? (size_t)dim * 8 : 0;   /* up to 32 KB, or 128 */ \
+        const size_t smem = partial != nullptr && (G::kGroups > 1 || kShared) ? (size_t)dim * 8 : 0;   /* up to 16 KB, or 128 */ \
         const int blocks = (rows - 1) / G::kGroups + 1, most = max_parts(dim);                                                 \
         *parts = blocks < most ? blocks : most;                                                                                \
         if (kShared) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * kMaxNormDim * (int)sizeof(float)); \
@@ -449,7 +449,7 @@ elsa_status launch_layer_norm_backward(const uint16_t* dY, const uint16_t* S, co
                                        cudaStream_t stream)
 {
     DeviceInfo dev;
-    elsa_status st = device_info(&dev);
+    elsa_status st = device_info(&dev);                // a device of another kind is refused
     if (st != ELSA_OK) return st;
     const RowShape shape = row_shape(dim);
     const float2* stats2 = reinterpret_cast<const float2*>(stats);
@@ -459,11 +459,11 @@ elsa_status launch_layer_norm_backward(const uint16_t* dY, const uint16_t* S, co
     {
         ProfileScope scope(ELSA_KERNEL_NORM_BACKWARD, stream);
         if (dtype == ELSA_BF16)
-            e = dS ? backward<true, true>(shape, dY, S, stats2, gain, dS, dX, partial, rows, dim, &parts, stream, dev)
-                   : backward<true, false>(shape, dY, S, stats2, gain, dS, dX, partial, rows, dim, &parts, stream, dev);
+            e = dS ? backward<true, true>(shape, dY, S, stats2, gain, dS, dX, partial, rows, dim, &parts, stream)
+                   : backward<true, false>(shape, dY, S, stats2, gain, dS, dX, partial, rows, dim, &parts, stream);
         else
-            e = dS ? backward<false, true>(shape, dY, S, stats2, gain, dS, dX, partial, rows, dim, &parts, stream, dev)
-                   : backward<false, false>(shape, dY, S, stats2, gain, dS, dX, partial, rows, dim, &parts, stream, dev);
+            e = dS ? backward<false, true>(shape, dY, S, stats2, gain, dS, dX, partial, rows, dim, &parts, stream)
+                   : backward<false, false>(shape, dY, S, stats2, gain, dS, dX, partial, rows, dim, &parts, stream);
         if (e != cudaSuccess) return fail(ELSA_ERR_CUDA, "layer_norm_backward launch: %s", cudaGetErrorString(e));
         if ((st = launched("layer_norm_backward")) != ELSA_OK || partial == nullptr) return st;
     }
