@@ -39,6 +39,10 @@ constexpr int kWalk = 64;                // walked rows of a tile
 // CTAs, where one's beginning and end run under the other's products, or three in one, which keep the tensor core busier once they
 // run: chosen by the sequences' mean length (12 heads of 64, us with one and with three: dq of 64 images of 49 to 1024 rows 191 and 224,
 // of 16 x 1024 132 and 136, of 6 x 2048 158 and 154; dk and dv of the images 230 and 240, of 32 x 512 97 and 101, of 16 x 1024 166 and 154).
+// The mean length stands for what an item walks, and is not the whole of it: heads of 32 cross at about 1400 and 1000 rows (16 x 1024 dq 112 and
+// 120, dk and dv 129 and 126; 12 x 1408 146 and 146, 169 and 159), under a causal mask both widths at 1400 to 2000 (heads of 64, 16 x 1024, dk and
+// dv 101 and 103; 8 x 2048 161 and 150), so there the two are within a tenth of one another; the group's heads are walked one after another, and
+// with 12 query heads on 3 key heads three stages are ahead from 512 rows on (89 and 73; causal 71 and 58), which the rule leaves to the other form.
 constexpr int kLongForQueries = 2048, kLongForKeys = 768;
 
 template <int kD, bool kKeys, int kGroupsOf>
